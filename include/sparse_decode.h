@@ -52,7 +52,7 @@ typedef enum {
   SD_ERR_HIP = -4           /* a HIP runtime call or kernel launch failed       */
 } sd_status;
 
-typedef enum { SD_F32 = 0, SD_BF16 = 1, SD_I32 = 2 } sd_dtype;
+typedef enum { SD_F32 = 0, SD_BF16 = 1, SD_I32 = 2, SD_U8 = 3 } sd_dtype;
 
 typedef enum {
   SD_KV_BHND = 0,      /* [B, Hkv, Ncap, d]: one contiguous slab per (sequence, KV head) */
@@ -335,6 +335,190 @@ sd_status sparse_decode_set_debug(int32_t flags);
  * reference for the bandwidth-bound kernels.  SD_ERR_INVALID_ARG for a null,
  * misaligned or empty buffer (checked before any HIP call). */
 sd_status sparse_decode_read_probe(const void *buf, size_t bytes, uint32_t *sink, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Attention with a sliding window and first tokens that stay visible.
+ *
+ * A query at position p sees the positions j <= p with j < n_sink or
+ * p - j < window: the first tokens of its sequence, its own position and the
+ * window - 1 before it.  window = INT32_MAX is causal attention over
+ * everything, window = 0 leaves the first tokens alone.  A query that sees
+ * nothing gives zeros. */
+typedef struct {
+  int32_t n_sink;        /* >= 0 */
+  int32_t window;        /* >= 0 */
+  float softmax_scale;   /* > 0, or <= 0 for 1/sqrt(128) */
+} sd_window;
+
+/*
+ * out[t, h] = sum over the positions j that query t sees of softmax(z)_j V_j,
+ * z_j = scale * q[t, h] . K_j, for one query per sequence or for several
+ * (chunks of a prompt, drafted tokens).
+ *   q        [T, Hq, 128], float32 or bfloat16, the dtype of K and V
+ *   seq_lens device int32 [batch]: positions in the cache, the queries' own
+ *            among them
+ *   q_starts NULL: T = batch, query t is sequence t's last position.
+ *            Else device int32 [batch + 1], ascending: sequence b's queries
+ *            are the rows [q_starts[b], q_starts[b + 1]) of q and its last
+ *            positions, the last row at position seq_lens[b] - 1.  Rows at
+ *            positions below 0 give zeros; rows of no sequence (behind
+ *            q_starts[batch], or before q_starts[0]) are left as they are.
+ *   batch    sequences: the rows of seq_lens (and of the block table)
+ *   out      [T, Hq, 128], dtype of q; may not overlap an input
+ * Positions that no query of the call sees are not read into any result,
+ * whatever they hold.  Positions on pages outside the pool (a block table
+ * entry below 0 or past its last page) are seen by no query.
+ * Uses sparse_decode_window_workspace_size bytes of the library workspace.
+ */
+sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,
+                                         const int32_t *seq_lens, const int32_t *q_starts,
+                                         int64_t batch, const sd_window *window, sd_tensor *out,
+                                         void *stream);
+sd_status sparse_decode_window_workspace_size(const sd_tensor *q, const sd_kv *K, int64_t batch,
+                                              int32_t packed, const sd_window *window,
+                                              size_t *bytes);
+
+/* ------------------------------------------------------------------------
+ * A key or value cache held in 4 bits.
+ *
+ * A row of 128 channels is 64 bytes of codes, channel 2i in the low half of
+ * byte i, and 4 scale bytes, one per 32 channels.  A code is a sign bit over
+ * an index into the levels 0, 0.5, 1, 1.5, 2, 3, 4, 6; scale byte s stands for
+ * 2^(s - 127), and 255 for a group that is not a number.  Layouts, head-major
+ * so that a head's rows lie in one run:
+ *   SD_KV_BHND       codes [B, Hkv, Ncap, 64],   scales [B, Hkv, Ncap, 4]
+ *   SD_KV_PAGED_NHD  codes [P, Hkv, 16, 64],     scales [P, Hkv, 16, 4]
+ * The block table and capacity are as in sd_kv. */
+typedef struct {
+  sd_tensor codes;               /* SD_U8, 16-byte aligned             */
+  sd_tensor scales;              /* SD_U8, 16-byte aligned             */
+  int32_t layout;                /* sd_kv_layout                       */
+  int32_t page_size;             /* paged: 16                          */
+  const int32_t *block_table;    /* paged: device int32 [batch, max_pages_per_seq] */
+  int32_t max_pages_per_seq;
+} sd_kv4;
+
+/*
+ * Write new keys and values into a 4-bit cache.  Group by group, with a the
+ * largest magnitude of its 32 channels, the scale is the smallest power of
+ * two 2^e with a < 7 * 2^e (7 is where the highest level, 6, is off by half a
+ * step), at least 2^-95; a channel takes the level nearest to x / 2^e,
+ * halfway cases the one of even index.  A group that holds a NaN or an
+ * infinity reads back as NaN.
+ *   k, v     [T, Hkv, 128], float32 or bfloat16 (both the same)
+ *   seq_lens device int32 [batch]: positions in the cache after the call,
+ *            the new ones among them
+ *   starts   as q_starts above: NULL writes row t at sequence t's last
+ *            position, else sequence b's rows [starts[b], starts[b + 1]) go
+ *            to its last positions.
+ * Rows at positions below 0, on pages outside the pool, or of no sequence, are
+ * not written.
+ */
+sd_status sparse_decode_q4_append(const sd_tensor *k, const sd_tensor *v, const sd_kv4 *K,
+                                  const sd_kv4 *V, const int32_t *seq_lens, const int32_t *starts,
+                                  int64_t batch, void *stream);
+
+/* The reverse: the last positions of each sequence as what they stand for
+ * (exact in both types).  k, v [T, Hkv, 128], written, float32 or bfloat16;
+ * rows and positions as in sparse_decode_q4_append.  Rows whose position is
+ * not in the cache (or whose page is not in the pool) are zeros, rows of no
+ * sequence are left as they are. */
+sd_status sparse_decode_q4_load(const sd_kv4 *K, const sd_kv4 *V, const int32_t *seq_lens,
+                                const int32_t *starts, int64_t batch, sd_tensor *k, sd_tensor *v,
+                                void *stream);
+
+/*
+ * Decode attention over a 4-bit cache: as sparse_decode_window_attention for
+ * one query per sequence, over the values that the cache stands for.
+ *   q      [B, Hq, 128] bfloat16 (float32 returns SD_ERR_UNSUPPORTED)
+ *   window NULL: every position of the sequence, scale 1/sqrt(128)
+ *   out    [B, Hq, 128] bfloat16
+ * Uses sparse_decode_q4_workspace_size bytes of the library workspace.
+ */
+sd_status sparse_decode_q4_attention(const sd_tensor *q, const sd_kv4 *K, const sd_kv4 *V,
+                                     const int32_t *seq_lens, const sd_window *window,
+                                     sd_tensor *out, void *stream);
+sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K,
+                                          const sd_window *window, size_t *bytes);
+
+/* ------------------------------------------------------------------------
+ * The pages of a paged cache.
+ *
+ * Sequence b holds the pages block_table[b, 0 .. ceil(seq_lens[b] / 16)), its
+ * other entries are -1.  refs[p] counts the rows that hold page p; 0 is a
+ * free page.  Full pages may be held by several rows, a part-filled last page
+ * by one, so that appending never writes into a shared page.  All three
+ * arrays are device memory that the calls below read and change; a pool is
+ * any tensor whose first dimension counts pages (keys, values, labels, 4-bit
+ * codes and scales).  Results do not depend on the order in which workgroups
+ * run.  Entries outside [0, n_pages) and lengths outside [0, 16 max_pages]
+ * (read as clamped to it) are memory-safe.  Calls that change the same arrays
+ * must be ordered on one stream. */
+typedef struct {
+  int32_t *block_table;  /* device int32 [batch, max_pages] */
+  int32_t *seq_lens;     /* device int32 [batch]            */
+  int32_t *refs;         /* device int32 [n_pages]          */
+  int64_t n_pages;
+  int32_t batch;
+  int32_t max_pages;
+} sd_pages;
+
+#define SD_MAX_POOLS 8
+
+/* Row b gets pages for grow[b] more positions (values below 0 count as 0),
+ * the lowest free pages first, in row order, and seq_lens[b] grows by them.
+ * status[b] (device int32 [batch], written): 0 = done; 1 = the free pages
+ * ended before this row had its own; 2 = more than max_pages pages.  Rows with
+ * a status other than 0 stay as they are; a row of status 1 uses up what it
+ * asked for, so that every later row that needs a page has status 1 too. */
+sd_status sparse_decode_pages_extend(const sd_pages *pages, const int32_t *grow, int32_t *status,
+                                     void *stream);
+
+/* Row i of `to` becomes a child of row parents[i] of `from` (parents: device
+ * int32 [to->batch]; a value outside [0, from->batch) makes an empty row).
+ * Children share the full pages of their parent and get a copy of its
+ * part-filled last page, in every pool, on a page of their own: the lowest
+ * free pages first, in row order.  What the rows of `to` held before is
+ * overwritten, not given back.
+ *   keep = 1: the parents stay as they are (parallel samples of one prompt).
+ *   keep = 0: the rows of `from` end with the call (a step of beam search):
+ *             a parent's first child takes its part-filled page over, the
+ *             pages of rows without children are given back, and every row of
+ *             `from` is left empty.
+ *   status    device int32 [to->batch], written: 0 = done; 1 = no free page
+ *             was left for the child's last page: the row is empty.
+ * `from` and `to` have the same refs, n_pages and max_pages; their tables and
+ * lengths may not overlap.  pools: n_pools (at most SD_MAX_POOLS) tensors of
+ * n_pages pages. */
+sd_status sparse_decode_pages_fork(const sd_pages *from, const sd_pages *to,
+                                   const int32_t *parents, int32_t keep, const sd_tensor *pools,
+                                   int32_t n_pools, int32_t *status, void *stream);
+
+/* The rows listed in rows (device int32 [n]; values outside [0, batch) are
+ * skipped, a row listed twice counts once) give back all their pages and are
+ * left empty. */
+sd_status sparse_decode_pages_free(const sd_pages *pages, const int32_t *rows, int64_t n,
+                                   void *stream);
+
+/* Page dst[i] = page src[i] of every pool (src, dst: device int32 [n]; pairs
+ * with a value outside the pools are skipped).  A page may not be both a
+ * source and a destination, nor a destination twice. */
+sd_status sparse_decode_pages_copy(const sd_tensor *pools, int32_t n_pools, const int32_t *src,
+                                   const int32_t *dst, int64_t n, void *stream);
+
+/* Move the live pages (refs > 0) together: with n of them, the i-th free page
+ * below n takes the content of the i-th live page from n on, in every pool, and
+ * block table and refs follow.
+ *   remap  device int32 [n_pages], written: where each page is now, -1 for
+ *          the pages that were free (for other tables of the same pools)
+ *   n_live device int32 [1], written: n */
+sd_status sparse_decode_pages_compact(const sd_pages *pages, const sd_tensor *pools,
+                                      int32_t n_pools, int32_t *remap, int32_t *n_live,
+                                      void *stream);
+
+/* Bytes of the library workspace that the calls above need for this pool and
+ * a table of at most `batch` rows. */
+sd_status sparse_decode_pages_workspace_size(int64_t n_pages, int64_t batch, size_t *bytes);
 
 const char *sparse_decode_status_string(sd_status status);
 

@@ -9,7 +9,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparse_decode.so")
-SOURCES = ["sd_api.hip", "sd_kernels.hip", "sd_dense.hip", "sd_probe.hip"]
+SOURCES = ["sd_kernels.hip", "sd_api.hip", "sd_dense.hip", "sd_probe.hip", "sd_token.hip",
+           "sd_chunk.hip", "sd_q4.hip", "sd_pages.hip"]
 ARCH = "gfx950"
 
 FLAGS = [

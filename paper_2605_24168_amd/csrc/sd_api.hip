@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "sparse_decode.h"
+#include "sd_cache.hpp"
 #include "sd_internal.hpp"
 #include "sd_launch.hpp"
 
@@ -1117,6 +1118,480 @@ sd_status sparse_decode_last_profile(sd_profile *out) { return summarize(out, nu
 
 sd_status sparse_decode_profile_mean(sd_profile *out, int32_t *n_calls) {
   return summarize(out, n_calls, true);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Window attention, the 4-bit cache, and pages.
+// ---------------------------------------------------------------------------
+namespace {
+
+bool aligned16(const void *p) { return (uintptr_t)p % 16 == 0; }
+
+// [T, heads, 128] of the given dtype; T may be 0.
+sd_status check_rows(const sd_tensor *t, int dtype, int64_t &rows, int64_t &heads) {
+  if (!t || t->ndim != 3 || t->dtype != dtype) return SD_ERR_INVALID_ARG;
+  if (t->shape[0] < 0 || t->shape[1] <= 0 || t->shape[2] <= 0) return SD_ERR_INVALID_ARG;
+  if (t->shape[2] != kHeadDim) return SD_ERR_UNSUPPORTED;
+  rows = t->shape[0];
+  heads = t->shape[1];
+  if (heads > 65535 || rows > INT32_MAX / 4 || rows * heads > INT32_MAX) return SD_ERR_UNSUPPORTED;
+  if (rows > 0 && (!t->data || !aligned16(t->data))) return SD_ERR_INVALID_ARG;
+  return SD_OK;
+}
+
+sd_status check_batch(int64_t batch) {
+  if (batch < 0) return SD_ERR_INVALID_ARG;
+  return batch > 65535 ? SD_ERR_UNSUPPORTED : SD_OK;
+}
+
+// Places of a cache's rows: its layout, capacity and pool.
+struct CacheShape {
+  int hkv = 0;
+  int64_t ncap = 0, pages = 0;
+  bool paged = false;
+};
+
+// data: the rows' tensor, whose last dimension is `row`; head_dim1: KV heads
+// are dimension 1 in the paged layout too (4-bit caches).
+sd_status check_cache(const sd_tensor &t, int layout, int page_size, const int32_t *block_table,
+                      int32_t max_pages, int64_t batch, int64_t row, bool heads_first,
+                      CacheShape &c) {
+  if (t.ndim != 4) return SD_ERR_INVALID_ARG;
+  bool empty = false;
+  for (int i = 0; i < 4; ++i) {
+    if (t.shape[i] < 0) return SD_ERR_INVALID_ARG;
+    empty = empty || t.shape[i] == 0;
+  }
+  if (t.shape[3] != row) return SD_ERR_UNSUPPORTED;
+  if (layout == SD_KV_BHND) {
+    if (t.shape[0] != batch) return SD_ERR_INVALID_ARG;
+    c.hkv = (int)t.shape[1];
+    c.ncap = t.shape[2];
+  } else if (layout == SD_KV_PAGED_NHD) {
+    if (page_size != sd::kTile) return SD_ERR_UNSUPPORTED;
+    if (t.shape[heads_first ? 2 : 1] != page_size) return SD_ERR_INVALID_ARG;
+    if (max_pages < 0 || (!block_table && max_pages > 0 && batch > 0)) return SD_ERR_INVALID_ARG;
+    if (t.shape[0] > INT32_MAX) return SD_ERR_UNSUPPORTED;
+    c.hkv = (int)t.shape[heads_first ? 1 : 2];
+    c.ncap = (int64_t)max_pages * page_size;
+    c.pages = t.shape[0];
+    c.paged = true;
+  } else {
+    return SD_ERR_INVALID_ARG;
+  }
+  if (c.hkv <= 0 || c.hkv > 65535) return SD_ERR_INVALID_ARG;
+  if (c.ncap > kMaxCapacity) return SD_ERR_UNSUPPORTED;
+  if (!empty && (!t.data || !aligned16(t.data))) return SD_ERR_INVALID_ARG;
+  if (c.paged && c.pages == 0) c.ncap = 0;  // no page to read: every sequence counts as empty
+  return SD_OK;
+}
+
+// Two caches that are addressed alike.
+bool same_shape(const CacheShape &a, const CacheShape &b) {
+  return a.hkv == b.hkv && a.ncap == b.ncap && a.pages == b.pages && a.paged == b.paged;
+}
+
+sd_status check_kv4(const sd_kv4 *kv, int64_t batch, CacheShape &c) {
+  if (!kv || kv->codes.dtype != SD_U8 || kv->scales.dtype != SD_U8) return SD_ERR_INVALID_ARG;
+  sd_status st = check_cache(kv->codes, kv->layout, kv->page_size, kv->block_table,
+                             kv->max_pages_per_seq, batch, sd::kQ4RowBytes, true, c);
+  if (st) return st;
+  CacheShape s;
+  st = check_cache(kv->scales, kv->layout, kv->page_size, kv->block_table, kv->max_pages_per_seq,
+                   batch, sd::kQ4Scales, true, s);
+  if (st) return st;
+  for (int i = 0; i < 3; ++i)
+    if (kv->codes.shape[i] != kv->scales.shape[i]) return SD_ERR_INVALID_ARG;
+  return SD_OK;
+}
+
+// A pair of caches: the same places, and in the paged layout one block table.
+sd_status check_pair4(const sd_kv4 *K, const sd_kv4 *V, int64_t batch, CacheShape &c) {
+  sd_status st = check_kv4(K, batch, c);
+  if (st) return st;
+  CacheShape v;
+  st = check_kv4(V, batch, v);
+  if (st) return st;
+  if (!same_shape(c, v) || (c.paged && K->block_table != V->block_table)) return SD_ERR_INVALID_ARG;
+  return SD_OK;
+}
+
+sd_status check_window(const sd_window *w) {
+  if (!w || w->n_sink < 0 || w->window < 0 || !std::isfinite(w->softmax_scale))
+    return SD_ERR_INVALID_ARG;
+  return SD_OK;
+}
+
+sd::WindowParams window_params(const CacheShape &c, int64_t batch, int64_t rows, int64_t hq,
+                               const sd_window *w) {
+  sd::WindowParams p{};
+  p.ncap = c.ncap;
+  p.n_rows = rows;
+  p.n_pages = (int32_t)c.pages;
+  p.max_pages = c.paged ? (int32_t)(c.ncap / sd::kTile) : 0;
+  p.batch = (int32_t)batch;
+  p.hq = (int32_t)hq;
+  p.hkv = c.hkv;
+  p.G = (int32_t)(hq / c.hkv);
+  p.n_sink = w ? w->n_sink : 0;
+  p.window = w ? w->window : INT32_MAX;
+  const float scale =
+      w && w->softmax_scale > 0.f ? w->softmax_scale : (float)(1.0 / std::sqrt((double)kHeadDim));
+  p.scale2 = (float)(scale * 1.4426950408889634);
+  return p;
+}
+
+size_t token_work_bytes(const sd::WindowParams &p) {
+  if (p.nsplit <= 1) return 0;
+  return align_up((size_t)p.batch * p.hq * p.nsplit * sd::kPartStride * sizeof(float));
+}
+
+// The checks that window attention and its workspace size share.
+sd_status check_window_call(const sd_tensor *q, const sd_kv *K, int64_t batch, bool packed,
+                            const sd_window *w, CacheShape &c, int64_t &rows, int64_t &hq) {
+  if (!q || !K || !is_dtype_float(q->dtype)) return SD_ERR_INVALID_ARG;
+  sd_status st = check_batch(batch);
+  if (!st) st = check_window(w);
+  if (!st) st = check_rows(q, q->dtype, rows, hq);
+  if (st) return st;
+  if (!packed && rows != batch) return SD_ERR_INVALID_ARG;
+  if (K->t.dtype != q->dtype) return SD_ERR_INVALID_ARG;
+  st = check_cache(K->t, K->layout, K->page_size, K->block_table, K->max_pages_per_seq, batch,
+                   kHeadDim, false, c);
+  if (st) return st;
+  if (hq % c.hkv) return SD_ERR_INVALID_ARG;
+  if (hq / c.hkv > sd::kMaxGroup) return SD_ERR_UNSUPPORTED;
+  return SD_OK;
+}
+
+// Splits and scratch of a decode call (one query per sequence).
+sd_status run_token(sd::WindowParams &p, int kind, bool paged, void *stream) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  DevState *ds = nullptr;
+  sd_status st = device_state(ds);
+  if (st) return st;
+  sd::window_split(p, kind);
+  if (p.nsplit > 1) {
+    char *base = nullptr;
+    st = get_workspace(token_work_bytes(p), ds, base);
+    if (st) return st;
+    p.part = (float *)base;
+  }
+  return hip_status(sd::launch_token_attend(p, kind, paged, (hipStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+sd_status sparse_decode_window_workspace_size(const sd_tensor *q, const sd_kv *K, int64_t batch,
+                                              int32_t packed, const sd_window *w, size_t *bytes) {
+  if (!bytes) return SD_ERR_INVALID_ARG;
+  CacheShape c;
+  int64_t rows = 0, hq = 0;
+  const sd_status st = check_window_call(q, K, batch, packed != 0, w, c, rows, hq);
+  if (st) return st;
+  *bytes = 0;
+  if (packed) return SD_OK;
+  sd::WindowParams p = window_params(c, batch, rows, hq, w);
+  sd::window_split(p, q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16);
+  *bytes = token_work_bytes(p);
+  return SD_OK;
+}
+
+sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,
+                                         const int32_t *seq_lens, const int32_t *q_starts,
+                                         int64_t batch, const sd_window *w, sd_tensor *out,
+                                         void *stream) {
+  CacheShape c, cv;
+  int64_t rows = 0, hq = 0, orows = 0, oh = 0;
+  sd_status st = check_window_call(q, K, batch, q_starts != nullptr, w, c, rows, hq);
+  if (st) return st;
+  if (!V || V->t.dtype != q->dtype || V->layout != K->layout) return SD_ERR_INVALID_ARG;
+  st = check_cache(V->t, V->layout, V->page_size, V->block_table, V->max_pages_per_seq, batch,
+                   kHeadDim, false, cv);
+  if (st) return st;
+  if (!same_shape(c, cv) || (c.paged && K->block_table != V->block_table)) return SD_ERR_INVALID_ARG;
+  st = check_rows(out, q->dtype, orows, oh);
+  if (st) return st;
+  if (orows != rows || oh != hq) return SD_ERR_INVALID_ARG;
+  if (rows == 0 || batch == 0) return SD_OK;
+  if (!seq_lens) return SD_ERR_INVALID_ARG;
+  sd::WindowParams p = window_params(c, batch, rows, hq, w);
+  p.q = q->data;
+  p.out = out->data;
+  p.k = (const char *)K->t.data;
+  p.v = (const char *)V->t.data;
+  p.block_table = K->block_table;
+  p.seq_lens = seq_lens;
+  p.q_starts = q_starts;
+  const int kind = q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16;
+  if (!q_starts) return run_token(p, kind, c.paged, stream);
+  return hip_status(sd::launch_chunk_attend(p, kind, c.paged, (hipStream_t)stream));
+}
+
+sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K, const sd_window *w,
+                                          size_t *bytes) {
+  if (!bytes || !q) return SD_ERR_INVALID_ARG;
+  if (q->dtype == SD_F32) return SD_ERR_UNSUPPORTED;
+  CacheShape c;
+  int64_t rows = 0, hq = 0;
+  sd_status st = check_rows(q, SD_BF16, rows, hq);
+  if (!st) st = check_batch(rows);
+  if (!st && w) st = check_window(w);
+  if (!st) st = check_kv4(K, rows, c);
+  if (st) return st;
+  if (hq % c.hkv) return SD_ERR_INVALID_ARG;
+  if (hq / c.hkv > sd::kMaxGroup) return SD_ERR_UNSUPPORTED;
+  sd::WindowParams p = window_params(c, rows, rows, hq, w);
+  sd::window_split(p, sd::kCacheQ4);
+  *bytes = token_work_bytes(p);
+  return SD_OK;
+}
+
+sd_status sparse_decode_q4_attention(const sd_tensor *q, const sd_kv4 *K, const sd_kv4 *V,
+                                     const int32_t *seq_lens, const sd_window *w, sd_tensor *out,
+                                     void *stream) {
+  size_t unused = 0;
+  sd_status st = sparse_decode_q4_workspace_size(q, K, w, &unused);
+  if (st) return st;
+  const int64_t batch = q->shape[0], hq = q->shape[1];
+  CacheShape c;
+  st = check_pair4(K, V, batch, c);
+  if (st) return st;
+  int64_t rows = 0, heads = 0;
+  st = check_rows(out, SD_BF16, rows, heads);
+  if (st) return st;
+  if (rows != batch || heads != hq) return SD_ERR_INVALID_ARG;
+  if (batch == 0) return SD_OK;
+  if (!seq_lens) return SD_ERR_INVALID_ARG;
+  sd::WindowParams p = window_params(c, batch, batch, hq, w);
+  p.q = q->data;
+  p.out = out->data;
+  p.k = (const char *)K->codes.data;
+  p.v = (const char *)V->codes.data;
+  p.ks = (const uint8_t *)K->scales.data;
+  p.vs = (const uint8_t *)V->scales.data;
+  p.block_table = K->block_table;
+  p.seq_lens = seq_lens;
+  return run_token(p, sd::kCacheQ4, c.paged, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Writing (append) or reading back (load) rows of a 4-bit cache.
+sd_status q4_rows(const sd_tensor *k, const sd_tensor *v, const sd_kv4 *K, const sd_kv4 *V,
+                  const int32_t *seq_lens, const int32_t *starts, int64_t batch, bool append,
+                  void *stream) {
+  if (!k || !v || !is_dtype_float(k->dtype)) return SD_ERR_INVALID_ARG;
+  sd_status st = check_batch(batch);
+  if (st) return st;
+  CacheShape c;
+  int64_t rows = 0, heads = 0, vrows = 0, vheads = 0;
+  st = check_rows(k, k->dtype, rows, heads);
+  if (!st) st = check_rows(v, k->dtype, vrows, vheads);
+  if (!st) st = check_pair4(K, V, batch, c);
+  if (st) return st;
+  if (rows != vrows || heads != vheads || heads != c.hkv) return SD_ERR_INVALID_ARG;
+  if (!starts && rows != batch) return SD_ERR_INVALID_ARG;
+  if (rows == 0 || batch == 0) return SD_OK;
+  if (!seq_lens) return SD_ERR_INVALID_ARG;
+  sd::Q4Params p{};
+  p.k = (uint8_t *)K->codes.data;
+  p.v = (uint8_t *)V->codes.data;
+  p.ks = (uint8_t *)K->scales.data;
+  p.vs = (uint8_t *)V->scales.data;
+  p.xk = k->data;
+  p.xv = v->data;
+  p.block_table = K->block_table;
+  p.seq_lens = seq_lens;
+  p.starts = starts;
+  p.ncap = c.ncap;
+  p.n_rows = rows;
+  p.n_pages = (int32_t)c.pages;
+  p.max_pages = c.paged ? K->max_pages_per_seq : 0;
+  p.batch = (int32_t)batch;
+  p.hkv = c.hkv;
+  const bool bf16 = k->dtype == SD_BF16;
+  return hip_status(append ? sd::launch_q4_append(p, bf16, c.paged, (hipStream_t)stream)
+                           : sd::launch_q4_load(p, bf16, c.paged, (hipStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+sd_status sparse_decode_q4_append(const sd_tensor *k, const sd_tensor *v, const sd_kv4 *K,
+                                  const sd_kv4 *V, const int32_t *seq_lens, const int32_t *starts,
+                                  int64_t batch, void *stream) {
+  return q4_rows(k, v, K, V, seq_lens, starts, batch, true, stream);
+}
+
+sd_status sparse_decode_q4_load(const sd_kv4 *K, const sd_kv4 *V, const int32_t *seq_lens,
+                                const int32_t *starts, int64_t batch, sd_tensor *k, sd_tensor *v,
+                                void *stream) {
+  return q4_rows(k, v, K, V, seq_lens, starts, batch, false, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kMaxPages = int64_t(1) << 28;
+
+sd_status check_pages(const sd_pages *p) {
+  if (!p || p->n_pages < 0 || p->batch < 0 || p->max_pages < 0) return SD_ERR_INVALID_ARG;
+  if (p->n_pages > kMaxPages || p->batch > 65535 || (int64_t)p->max_pages * sd::kTile > kMaxCapacity)
+    return SD_ERR_UNSUPPORTED;
+  if (p->n_pages > 0 && !p->refs) return SD_ERR_INVALID_ARG;
+  if (p->batch > 0 && (!p->seq_lens || (p->max_pages > 0 && !p->block_table)))
+    return SD_ERR_INVALID_ARG;
+  return SD_OK;
+}
+
+sd::PagesParams pages_params(const sd_pages *p) {
+  return sd::PagesParams{p->block_table, p->seq_lens, p->refs, (int32_t)p->n_pages, p->batch,
+                         p->max_pages};
+}
+
+int dtype_bytes(int32_t d) {
+  return d == SD_F32 || d == SD_I32 ? 4 : (d == SD_BF16 ? 2 : (d == SD_U8 ? 1 : 0));
+}
+
+// n_pages: of every pool (set from the first one when it is negative).
+sd_status check_pools(const sd_tensor *pools, int32_t n, int64_t &n_pages, sd::Pools &out) {
+  static_assert(sd::kMaxPools == SD_MAX_POOLS, "pools");
+  if (n < 0 || (n > 0 && !pools)) return SD_ERR_INVALID_ARG;
+  if (n > SD_MAX_POOLS) return SD_ERR_UNSUPPORTED;
+  out = sd::Pools{};
+  out.align = 16;
+  for (int i = 0; i < n; ++i) {
+    const sd_tensor &t = pools[i];
+    const int size = dtype_bytes(t.dtype);
+    if (size == 0 || t.ndim < 1 || t.ndim > 4 || t.shape[0] < 0) return SD_ERR_INVALID_ARG;
+    if (n_pages < 0) n_pages = t.shape[0];
+    if (t.shape[0] != n_pages) return SD_ERR_INVALID_ARG;
+    int64_t bytes = size;
+    for (int d = 1; d < t.ndim; ++d) {
+      if (t.shape[d] < 0) return SD_ERR_INVALID_ARG;
+      bytes *= t.shape[d];
+      if (bytes > (int64_t(1) << 30)) return SD_ERR_UNSUPPORTED;
+    }
+    if (bytes == 0 || n_pages == 0) continue;
+    if (!t.data) return SD_ERR_INVALID_ARG;
+    while ((uintptr_t)t.data % out.align || bytes % out.align) out.align /= 2;
+    out.base[out.n] = (char *)t.data;
+    out.page_bytes[out.n] = bytes;
+    ++out.n;
+  }
+  if (n_pages > kMaxPages) return SD_ERR_UNSUPPORTED;
+  return SD_OK;
+}
+
+bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return na && nb && x < y + nb && y < x + na;
+}
+
+// The workspace of the page calls, as f(base).
+template <class F>
+sd_status with_pages_work(int64_t n_pages, int64_t batch, F f) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  DevState *ds = nullptr;
+  char *base = nullptr;
+  const sd_status st = get_workspace(sd::pages_work_bytes(n_pages, batch), ds, base);
+  return st ? st : hip_status(f(base));
+}
+
+}  // namespace
+
+extern "C" {
+
+sd_status sparse_decode_pages_workspace_size(int64_t n_pages, int64_t batch, size_t *bytes) {
+  if (!bytes || n_pages < 0 || batch < 0) return SD_ERR_INVALID_ARG;
+  if (n_pages > kMaxPages || batch > 65535) return SD_ERR_UNSUPPORTED;
+  *bytes = sd::pages_work_bytes(n_pages, batch);
+  return SD_OK;
+}
+
+sd_status sparse_decode_pages_extend(const sd_pages *pages, const int32_t *grow, int32_t *status,
+                                     void *stream) {
+  const sd_status st = check_pages(pages);
+  if (st) return st;
+  if (pages->batch == 0) return SD_OK;
+  if (!grow || !status) return SD_ERR_INVALID_ARG;
+  return with_pages_work(pages->n_pages, pages->batch, [&](char *base) {
+    return sd::launch_pages_extend(pages_params(pages), grow, status, base, (hipStream_t)stream);
+  });
+}
+
+sd_status sparse_decode_pages_fork(const sd_pages *from, const sd_pages *to,
+                                   const int32_t *parents, int32_t keep, const sd_tensor *pools,
+                                   int32_t n_pools, int32_t *status, void *stream) {
+  sd_status st = check_pages(from);
+  if (!st) st = check_pages(to);
+  if (st) return st;
+  if (keep != 0 && keep != 1) return SD_ERR_INVALID_ARG;
+  if (from->refs != to->refs || from->n_pages != to->n_pages || from->max_pages != to->max_pages)
+    return SD_ERR_INVALID_ARG;
+  const size_t row = 4 * (size_t)from->max_pages;
+  if (overlap(from->block_table, row * from->batch, to->block_table, row * to->batch) ||
+      overlap(from->seq_lens, 4 * (size_t)from->batch, to->seq_lens, 4 * (size_t)to->batch))
+    return SD_ERR_INVALID_ARG;
+  int64_t n_pages = from->n_pages;
+  sd::Pools pl;
+  st = check_pools(pools, n_pools, n_pages, pl);
+  if (st) return st;
+  if (from->batch == 0 && to->batch == 0) return SD_OK;
+  if (to->batch > 0 && (!parents || !status)) return SD_ERR_INVALID_ARG;
+  return with_pages_work(n_pages, std::max(from->batch, to->batch), [&](char *base) {
+    return sd::launch_pages_fork(pages_params(from), pages_params(to), parents, keep != 0, pl,
+                                 status, base, (hipStream_t)stream);
+  });
+}
+
+sd_status sparse_decode_pages_free(const sd_pages *pages, const int32_t *rows, int64_t n,
+                                   void *stream) {
+  const sd_status st = check_pages(pages);
+  if (st) return st;
+  if (n < 0) return SD_ERR_INVALID_ARG;
+  if (n > INT32_MAX) return SD_ERR_UNSUPPORTED;
+  if (n == 0 || pages->batch == 0) return SD_OK;
+  if (!rows) return SD_ERR_INVALID_ARG;
+  return hip_status(sd::launch_pages_free(pages_params(pages), rows, n, (hipStream_t)stream));
+}
+
+sd_status sparse_decode_pages_copy(const sd_tensor *pools, int32_t n_pools, const int32_t *src,
+                                   const int32_t *dst, int64_t n, void *stream) {
+  int64_t n_pages = -1;
+  sd::Pools pl;
+  const sd_status st = check_pools(pools, n_pools, n_pages, pl);
+  if (st) return st;
+  if (n < 0) return SD_ERR_INVALID_ARG;
+  if (n > INT32_MAX) return SD_ERR_UNSUPPORTED;
+  if (n == 0 || pl.n == 0) return SD_OK;
+  if (!src || !dst) return SD_ERR_INVALID_ARG;
+  return hip_status(sd::launch_pages_copy(pl, n_pages, src, dst, n, (hipStream_t)stream));
+}
+
+sd_status sparse_decode_pages_compact(const sd_pages *pages, const sd_tensor *pools,
+                                      int32_t n_pools, int32_t *remap, int32_t *n_live,
+                                      void *stream) {
+  sd_status st = check_pages(pages);
+  if (st) return st;
+  int64_t n_pages = pages->n_pages;
+  sd::Pools pl;
+  st = check_pools(pools, n_pools, n_pages, pl);
+  if (st) return st;
+  if (!n_live || (n_pages > 0 && !remap)) return SD_ERR_INVALID_ARG;
+  return with_pages_work(n_pages, pages->batch, [&](char *base) {
+    return sd::launch_pages_compact(pages_params(pages), pl, remap, n_live, base,
+                                    (hipStream_t)stream);
+  });
 }
 
 }  // extern "C"

@@ -1,0 +1,98 @@
+// sd_cache.hpp -- what the kernels of window attention, of the 4-bit cache and
+// of the pages share: their parameters and host launchers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "sd_internal.hpp"
+
+namespace sd {
+
+// How a cache holds its rows.
+enum CacheKind { kCacheF32 = 0, kCacheBf16 = 1, kCacheQ4 = 2 };
+
+constexpr int kQ4RowBytes = kHeadDim / 2;  // codes of a row
+constexpr int kQ4Group = 32;               // channels that share a scale
+constexpr int kQ4Scales = kHeadDim / kQ4Group;
+constexpr int kQ4MinScale = 32;            // smallest scale byte written: 2^-95
+constexpr int kQ4NanScale = 255;
+
+// Attention over the positions that windows and first tokens leave visible.
+struct WindowParams {
+  const void *q;               // [T, Hq, 128]
+  void *out;                   // [T, Hq, 128]
+  const char *k, *v;           // rows, or codes
+  const uint8_t *ks, *vs;      // 4-bit caches: scale bytes
+  const int32_t *block_table;  // paged: [batch, max_pages]
+  const int32_t *seq_lens;     // [batch]
+  const int32_t *q_starts;     // [batch + 1]; null: one query per sequence
+  float *part;                 // [T * Hq][nsplit][kPartStride], see k_token_merge
+  int64_t ncap;                // positions addressable per sequence
+  int64_t n_rows;              // T
+  int32_t n_pages;             // pages of the pool
+  int32_t max_pages;
+  int32_t batch, hq, hkv, G;
+  int32_t n_sink, window;
+  float scale2;                // softmax scale times log2(e)
+  int32_t span;                // tiles of 16 positions per split
+  int32_t nsplit;
+};
+
+// Splits of one sequence and KV head over workgroups, from what the host
+// knows (see window_split); fills p.span and p.nsplit.
+void window_split(WindowParams &p, int kind);
+hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
+hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
+
+// Writing and reading a 4-bit cache.
+struct Q4Params {
+  uint8_t *k, *v, *ks, *vs;    // codes and scale bytes
+  void *xk, *xv;               // rows [T, Hkv, 128], float32 or bfloat16
+  const int32_t *block_table;
+  const int32_t *seq_lens;
+  const int32_t *starts;
+  int64_t ncap, n_rows;
+  int32_t n_pages, max_pages, batch, hkv;
+};
+hipError_t launch_q4_append(const Q4Params &p, bool bf16, bool paged, hipStream_t st);
+hipError_t launch_q4_load(const Q4Params &p, bool bf16, bool paged, hipStream_t st);
+
+// Pages.
+constexpr int kMaxPools = 8;
+struct Pools {
+  char *base[kMaxPools];
+  int64_t page_bytes[kMaxPools];
+  int32_t n;
+  int32_t align;               // largest power of two up to 16 that divides every address and size
+};
+struct PagesParams {
+  int32_t *table, *seq_lens, *refs;
+  int32_t n_pages, batch, max_pages;
+};
+size_t pages_work_bytes(int64_t n_pages, int64_t batch);
+hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_t *status,
+                               char *work, hipStream_t st);
+hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
+                             const int32_t *parents, bool keep, const Pools &pools,
+                             int32_t *status, char *work, hipStream_t st);
+hipError_t launch_pages_free(const PagesParams &p, const int32_t *rows, int64_t n, hipStream_t st);
+hipError_t launch_pages_copy(const Pools &pools, int64_t n_pages, const int32_t *src,
+                             const int32_t *dst, int64_t n, hipStream_t st);
+hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_t *remap,
+                                int32_t *n_live, char *work, hipStream_t st);
+
+// Sequence length, clamped to the capacity.
+__device__ __forceinline__ int clamp_len(const int32_t *seq_lens, int b, int64_t ncap) {
+  int64_t L = seq_lens[b];
+  L = L < 0 ? 0 : L;
+  return (int)(L > ncap ? ncap : L);
+}
+
+// starts[i] of [0, batch], clamped to [0, n_rows] (null: one row each).
+__device__ __forceinline__ int64_t clamp_start(const int32_t *starts, int i, int64_t n_rows) {
+  if (!starts) return i;
+  const int64_t s = starts[i];
+  return s < 0 ? 0 : (s > n_rows ? n_rows : s);
+}
+
+}  // namespace sd

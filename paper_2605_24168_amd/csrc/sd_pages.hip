@@ -1,0 +1,498 @@
+// sd_pages.hip -- the pages of a paged cache: extending and freeing rows of a
+// block table, forking rows, copying pages, and moving live pages together.
+//
+// The tables and counts are small, so these are bound by launches and by the
+// latency of a few dependent reads; only the copies move bytes that matter.
+// Free pages are taken lowest first, which makes results independent of the
+// order of workgroups: a first kernel counts the free pages of every stretch
+// of the pool, one workgroup turns counts and requests into ranks, and a third
+// hands the free pages out by rank.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "sd_cache.hpp"
+#include "sd_internal.hpp"
+
+namespace sd {
+
+constexpr int kStretch = 4096;                    // pages counted by one workgroup
+constexpr int kPerThread = kStretch / kBlock;     // consecutive pages of a thread
+constexpr int kPlan = 1024;                       // threads of the planning workgroup
+constexpr int64_t kPiece = 16 * 1024;             // bytes a workgroup copies at once
+constexpr int kMany = 1 << 29;                    // more than any number of pages
+
+// Scratch of one call (all int32).
+struct PageWork {
+  int32_t *base;      // [stretches]: counts, then the free (or live) pages before each
+  int32_t *scalar;    // [8]: see kLimit ...
+  int32_t *first;     // [batch]: extend: rank of the row's first page
+  int32_t *have;      // [batch]: extend: pages it held; fork: children of a parent
+  int32_t *eldest;    // [batch]: fork: a parent's first child
+  int32_t *list;      // [pages]: fork: child of each rank; compact: movers
+  int32_t *hole;      // [pages]: compact: holes; fork: [0, batch) fresh pages, [batch, ..) old ones
+};
+enum { kLimit = 0, kMoves = 1, kLive = 2 };
+
+static inline int64_t stretches(int64_t n_pages) { return (n_pages + kStretch - 1) / kStretch; }
+
+static inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+static size_t carve_pages(int64_t n_pages, int64_t batch, char *base, PageWork *w) {
+  size_t at = 0;
+  auto take = [&](int64_t n) {
+    char *ptr = base ? base + at : nullptr;
+    at += up256(4 * (size_t)n);
+    return (int32_t *)ptr;
+  };
+  PageWork x;
+  x.base = take(stretches(n_pages));
+  x.scalar = take(8);
+  x.first = take(batch);
+  x.have = take(batch);
+  x.eldest = take(batch);
+  x.list = take(n_pages > batch ? n_pages : batch);
+  x.hole = take(n_pages > 2 * batch ? n_pages : 2 * batch);
+  if (w) *w = x;
+  return at;
+}
+
+size_t pages_work_bytes(int64_t n_pages, int64_t batch) {
+  return carve_pages(n_pages, batch, nullptr, nullptr);
+}
+
+__device__ __forceinline__ int row_len(const PagesParams &p, int b) {
+  return clamp_len(p.seq_lens, b, (int64_t)p.max_pages * kTile);
+}
+__device__ __forceinline__ bool in_pool(const PagesParams &p, int page) {
+  return page >= 0 && page < p.n_pages;
+}
+
+// This thread's pages of stretch `s`: a bit for each that is free (or live).
+template <bool LIVE>
+__device__ __forceinline__ uint32_t stretch_bits(const PagesParams &p, int s) {
+  const int64_t i0 = (int64_t)s * kStretch + threadIdx.x * kPerThread;
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
+    const int64_t page = i0 + i;
+    if (page < p.n_pages && (LIVE ? p.refs[page] > 0 : p.refs[page] == 0)) m |= 1u << i;
+  }
+  return m;
+}
+
+template <bool LIVE>
+__global__ __launch_bounds__(kBlock) void k_pages_count(PagesParams p, PageWork w) {
+  __shared__ int tmp[kWaves];
+  int total;
+  block_excl_scan(__popc(stretch_bits<LIVE>(p, blockIdx.x)), tmp, &total);
+  if (threadIdx.x == 0) w.base[blockIdx.x] = total;
+}
+
+// Counts of the stretches to the pages before each; returns all of them.
+__device__ __forceinline__ int plan_bases(const PageWork &w, int n, int *tmp) {
+  int before = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlan) {
+    const int i = i0 + threadIdx.x;
+    const int c = i < n ? w.base[i] : 0;
+    int total;
+    const int x = block_excl_scan<kPlan>(c, tmp, &total);
+    if (i < n) w.base[i] = before + x;
+    before += total;
+  }
+  return before;
+}
+
+// ---------------------------------------------------------------------------
+// extend
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kPlan) void k_extend_plan(PagesParams p, PageWork w,
+                                                       const int32_t *grow, int32_t *status) {
+  __shared__ int tmp[kPlan / 64];
+  __shared__ int limit;
+  const int nfree = plan_bases(w, (int)((p.n_pages + kStretch - 1) / kStretch), tmp);
+  if (threadIdx.x == 0) limit = 0;
+  __syncthreads();
+  int before = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kPlan) {
+    const int b = b0 + threadIdx.x;
+    int need = 0, have = 0;
+    int64_t L = 0;
+    bool fits = true;
+    if (b < p.batch) {
+      L = row_len(p, b);
+      have = (int)((L + kTile - 1) / kTile);
+      const int64_t g = grow[b];
+      L += g > 0 ? g : 0;
+      const int64_t want = (L + kTile - 1) / kTile;
+      fits = want <= p.max_pages;
+      need = fits ? (int)want - have : 0;
+    }
+    int total;
+    const int first = before + block_excl_scan<kPlan>(need, tmp, &total);
+    if (b < p.batch) {
+      const bool ok = fits && (need == 0 || first + need <= nfree);
+      status[b] = !fits ? 2 : (ok ? 0 : 1);
+      if (ok) p.seq_lens[b] = (int32_t)L;
+      w.first[b] = first;
+      w.have[b] = have;
+      if (ok && need > 0) atomicMax(&limit, first + need);
+    }
+    before = min(before + total, kMany);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) w.scalar[kLimit] = limit;
+}
+
+// Rows that get pages are those whose ranks end at or below the limit; their
+// ranks ascend, so a free page finds its row by bisection.
+__global__ __launch_bounds__(kBlock) void k_extend_take(PagesParams p, PageWork w) {
+  __shared__ int tmp[kWaves];
+  const int limit = w.scalar[kLimit];
+  const int base = w.base[blockIdx.x];
+  if (base >= limit) return;
+  const uint32_t mine = stretch_bits<false>(p, blockIdx.x);
+  int total;
+  int rank = base + block_excl_scan(__popc(mine), tmp, &total);
+  for (uint32_t m = mine; m && rank < limit; m &= m - 1, ++rank) {
+    const int page = (int)blockIdx.x * kStretch + threadIdx.x * kPerThread + __ffs(m) - 1;
+    int lo = 0, hi = p.batch;  // first row whose ranks start past this one
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (w.first[mid] <= rank) lo = mid + 1;
+      else hi = mid;
+    }
+    const int b = lo - 1;
+    p.table[(int64_t)b * p.max_pages + w.have[b] + rank - w.first[b]] = page;
+    p.refs[page] = 1;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// fork
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kPlan) void k_fork_plan(PagesParams from, PagesParams to, PageWork w,
+                                                     const int32_t *parents, int keep,
+                                                     int32_t *status) {
+  __shared__ int tmp[kPlan / 64];
+  const int nfree = plan_bases(w, (int)((from.n_pages + kStretch - 1) / kStretch), tmp);
+  for (int r = threadIdx.x; r < from.batch; r += kPlan) {
+    w.have[r] = 0;
+    w.eldest[r] = INT32_MAX;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < to.batch; i += kPlan) {
+    const int r = parents[i];
+    if (r >= 0 && r < from.batch) atomicMin(&w.eldest[r], i);
+  }
+  __syncthreads();
+  int32_t *fresh = w.hole, *old = w.hole + to.batch;
+  int before = 0;
+  for (int i0 = 0; i0 < to.batch; i0 += kPlan) {
+    const int i = i0 + threadIdx.x;
+    int r = -1, L = 0;
+    bool need = false;
+    if (i < to.batch) {
+      r = parents[i];
+      if (r < 0 || r >= from.batch) r = -1;
+      if (r >= 0) {
+        L = row_len(from, r);
+        need = L % kTile != 0 && (keep || __hip_atomic_load(&w.eldest[r], __ATOMIC_RELAXED,
+                                                              __HIP_MEMORY_SCOPE_WORKGROUP) != i);
+      }
+    }
+    int total;
+    const int rank = before + block_excl_scan<kPlan>(need ? 1 : 0, tmp, &total);
+    if (i < to.batch) {
+      const bool ok = !need || rank < nfree;
+      status[i] = ok ? 0 : 1;
+      to.seq_lens[i] = ok ? L : 0;
+      fresh[i] = -1;
+      old[i] = need ? from.table[(int64_t)r * from.max_pages + L / kTile] : -1;
+      if (need && ok) w.list[rank] = i;
+      if (ok && r >= 0) atomicAdd(&w.have[r], 1);
+      // (what k_fork_rows makes of the row: its parent, or none)
+      w.first[i] = ok ? r : -1;
+    }
+    before += total;
+  }
+  if (threadIdx.x == 0) w.scalar[kLimit] = min(before, nfree);
+}
+
+__global__ __launch_bounds__(kBlock) void k_fork_take(PagesParams p, PageWork w) {
+  __shared__ int tmp[kWaves];
+  const int limit = w.scalar[kLimit];
+  const int base = w.base[blockIdx.x];
+  if (base >= limit) return;
+  const uint32_t mine = stretch_bits<false>(p, blockIdx.x);
+  int total;
+  int rank = base + block_excl_scan(__popc(mine), tmp, &total);
+  for (uint32_t m = mine; m && rank < limit; m &= m - 1, ++rank) {
+    const int page = (int)blockIdx.x * kStretch + threadIdx.x * kPerThread + __ffs(m) - 1;
+    w.hole[w.list[rank]] = page;
+    p.refs[page] = 1;
+  }
+}
+
+// Workgroups [0, to.batch) write the children's rows, the others count the
+// parents' pages.
+__global__ __launch_bounds__(kBlock) void k_fork_rows(PagesParams from, PagesParams to, PageWork w,
+                                                      int keep) {
+  const int i = blockIdx.x;
+  if (i < to.batch) {
+    const int r = w.first[i];
+    const int L = r >= 0 ? row_len(from, r) : 0;
+    const int full = L / kTile, n = (L + kTile - 1) / kTile;
+    const int fresh = w.hole[i];
+    int32_t *dst = to.table + (int64_t)i * to.max_pages;
+    const int32_t *src = from.table + (int64_t)(r < 0 ? 0 : r) * from.max_pages;
+    for (int c = threadIdx.x; c < to.max_pages; c += kBlock) {
+      int page = -1;
+      if (c < n) page = c == full && fresh >= 0 ? fresh : src[c];
+      dst[c] = page;
+    }
+    return;
+  }
+  const int r = i - to.batch;
+  const int L = row_len(from, r), children = w.have[r];
+  const int32_t *src = from.table + (int64_t)r * from.max_pages;
+  const int delta = keep ? children : children - 1;
+  if (delta != 0)
+    for (int c = threadIdx.x; c < L / kTile; c += kBlock)
+      if (in_pool(from, src[c])) atomicAdd(&from.refs[src[c]], delta);
+  if (!keep && children == 0 && L % kTile && threadIdx.x == 0) {
+    const int page = src[L / kTile];
+    if (in_pool(from, page)) atomicAdd(&from.refs[page], -1);
+  }
+}
+
+// Pieces of a page over all pools.
+__host__ __device__ static inline int pieces_of(const Pools &pools) {
+  int n = 0;
+  for (int i = 0; i < pools.n; ++i) n += (int)((pools.page_bytes[i] + kPiece - 1) / kPiece);
+  return n;
+}
+
+template <class T>
+__device__ __forceinline__ void copy_run(const char *src, char *dst, int64_t bytes) {
+  constexpr int U = 4;
+  const int64_t n = bytes / (int64_t)sizeof(T);
+  for (int64_t i0 = 0; i0 < n; i0 += kBlock * U) {
+    T x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * kBlock + threadIdx.x;
+      if (i < n) x[u] = __builtin_nontemporal_load((const T *)src + i);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * kBlock + threadIdx.x;
+      if (i < n) __builtin_nontemporal_store(x[u], (T *)dst + i);
+    }
+  }
+}
+
+// Piece `k` of page src to page dst.
+__device__ __forceinline__ void copy_piece(const Pools &pools, int64_t src, int64_t dst, int k) {
+  for (int i = 0; i < pools.n; ++i) {
+    const int64_t bytes = pools.page_bytes[i];
+    const int n = (int)((bytes + kPiece - 1) / kPiece);
+    if (k < n) {
+      const int64_t at = k * kPiece, len = bytes - at < kPiece ? bytes - at : kPiece;
+      const char *s = pools.base[i] + src * bytes + at;
+      char *d = pools.base[i] + dst * bytes + at;
+      if (pools.align == 16) copy_run<u32x4>(s, d, len);
+      else if (pools.align >= 4) copy_run<uint32_t>(s, d, len);
+      else copy_run<uint8_t>(s, d, len);
+      return;
+    }
+    k -= n;
+  }
+}
+
+// Workgroups [0, to.batch * pieces) copy the part-filled pages, the others
+// empty the rows that the call ends.
+__global__ __launch_bounds__(kBlock) void k_fork_tails(PagesParams from, PagesParams to, PageWork w,
+                                                       Pools pools, int pieces) {
+  const int64_t i = blockIdx.x;
+  if (i < (int64_t)to.batch * pieces) {
+    const int child = (int)(i / pieces);
+    const int fresh = w.hole[child], old = w.hole[to.batch + child];
+    if (fresh >= 0 && in_pool(from, old)) copy_piece(pools, old, fresh, (int)(i % pieces));
+    return;
+  }
+  const int r = (int)(i - (int64_t)to.batch * pieces);
+  int32_t *row = from.table + (int64_t)r * from.max_pages;
+  for (int c = threadIdx.x; c < from.max_pages; c += kBlock) row[c] = -1;
+  if (threadIdx.x == 0) from.seq_lens[r] = 0;
+}
+
+// ---------------------------------------------------------------------------
+// free, copy
+// ---------------------------------------------------------------------------
+// An entry is exchanged for -1, so that a row listed twice gives its pages
+// back once.
+__global__ __launch_bounds__(kBlock) void k_pages_free(PagesParams p, const int32_t *rows) {
+  const int b = rows[blockIdx.x];
+  if (b < 0 || b >= p.batch) return;
+  int32_t *row = p.table + (int64_t)b * p.max_pages;
+  for (int c = threadIdx.x; c < p.max_pages; c += kBlock) {
+    const int page = atomicExch(&row[c], -1);
+    if (in_pool(p, page)) atomicAdd(&p.refs[page], -1);
+  }
+  if (threadIdx.x == 0) p.seq_lens[b] = 0;
+}
+
+__global__ __launch_bounds__(kBlock) void k_pages_copy(Pools pools, int64_t n_pages,
+                                                       const int32_t *src, const int32_t *dst,
+                                                       int pieces) {
+  const int64_t i = blockIdx.x / pieces;
+  const int64_t s = src[i], d = dst[i];
+  if (s < 0 || s >= n_pages || d < 0 || d >= n_pages || s == d) return;
+  copy_piece(pools, s, d, (int)(blockIdx.x % pieces));
+}
+
+// ---------------------------------------------------------------------------
+// compact
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kPlan) void k_compact_plan(PagesParams p, PageWork w, int32_t *n_live) {
+  __shared__ int tmp[kPlan / 64];
+  const int n = plan_bases(w, (int)((p.n_pages + kStretch - 1) / kStretch), tmp);
+  // Live pages below n: those of the stretches before n's, and of its own.
+  __syncthreads();
+  const int s = n / kStretch;
+  int c = 0;
+  for (int64_t i = (int64_t)s * kStretch + threadIdx.x; i < n; i += kPlan) c += p.refs[i] > 0;
+  int total;
+  block_excl_scan<kPlan>(c, tmp, &total);
+  if (threadIdx.x == 0) {
+    const int64_t last = (p.n_pages + kStretch - 1) / kStretch;
+    const int below = (s < last ? w.base[s] : n) + total;
+    w.scalar[kLive] = n;
+    w.scalar[kMoves] = n - below;
+    *n_live = n;
+  }
+}
+
+// Movers and holes in ascending order; a mover's entry of remap holds its rank
+// i as -2 - i until k_compact_move has put the page there.
+__global__ __launch_bounds__(kBlock) void k_compact_lists(PagesParams p, PageWork w, int32_t *remap) {
+  __shared__ int tmp[kWaves];
+  const int n = w.scalar[kLive], below = n - w.scalar[kMoves];
+  const uint32_t mine = stretch_bits<true>(p, blockIdx.x);
+  int total;
+  int live = w.base[blockIdx.x] + block_excl_scan(__popc(mine), tmp, &total);
+  const int64_t p0 = (int64_t)blockIdx.x * kStretch + threadIdx.x * kPerThread;
+  for (int i = 0; i < kPerThread; ++i) {
+    const int64_t page = p0 + i;
+    if (page >= p.n_pages) return;
+    if (mine >> i & 1) {
+      if (page < n) {
+        remap[page] = (int)page;
+      } else {
+        w.list[live - below] = (int)page;
+        remap[page] = -2 - (live - below);
+      }
+      ++live;
+    } else {
+      remap[page] = -1;
+      if (page < n) w.hole[page - live] = (int)page;
+    }
+  }
+}
+
+// The table first (workgroups [0, batch)): an entry reads its page's rank or,
+// once that is written, its new place.  Then counts and remap by rank, then
+// the pages themselves.
+__global__ __launch_bounds__(kBlock) void k_compact_move(PagesParams p, PageWork w, Pools pools,
+                                                         int32_t *remap, int pieces, int counters) {
+  const int moves = w.scalar[kMoves];
+  int64_t i = blockIdx.x;
+  if (i < p.batch) {
+    int32_t *row = p.table + i * p.max_pages;
+    for (int c = threadIdx.x; c < p.max_pages; c += kBlock) {
+      const int page = row[c];
+      if (!in_pool(p, page)) continue;
+      const int to = __hip_atomic_load(&remap[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (to != page) row[c] = to <= -2 ? w.hole[-2 - to] : to;
+    }
+    return;
+  }
+  i -= p.batch;
+  if (i < counters) {
+    for (int64_t k = i * kBlock + threadIdx.x; k < moves; k += (int64_t)counters * kBlock) {
+      const int from = w.list[k], to = w.hole[k];
+      p.refs[to] = p.refs[from];
+      p.refs[from] = 0;
+      __hip_atomic_store(&remap[from], to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    return;
+  }
+  i -= counters;
+  const int64_t movers = (int64_t)gridDim.x - p.batch - counters;
+  for (int64_t k = i; k < (int64_t)moves * pieces; k += movers)
+    copy_piece(pools, w.list[k / pieces], w.hole[k / pieces], (int)(k % pieces));
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_t *status,
+                               char *work, hipStream_t st) {
+  PageWork w;
+  carve_pages(p.n_pages, p.batch, work, &w);
+  const unsigned n = (unsigned)stretches(p.n_pages);
+  if (n) k_pages_count<false><<<n, kBlock, 0, st>>>(p, w);
+  k_extend_plan<<<1, kPlan, 0, st>>>(p, w, grow, status);
+  if (n) k_extend_take<<<n, kBlock, 0, st>>>(p, w);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
+                             const int32_t *parents, bool keep, const Pools &pools,
+                             int32_t *status, char *work, hipStream_t st) {
+  PageWork w;
+  carve_pages(from.n_pages, from.batch > to.batch ? from.batch : to.batch, work, &w);
+  const unsigned n = (unsigned)stretches(from.n_pages);
+  const int pieces = pieces_of(pools);
+  const int64_t tails = (int64_t)to.batch * pieces + (keep ? 0 : from.batch);
+  if (tails > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (n) k_pages_count<false><<<n, kBlock, 0, st>>>(from, w);
+  k_fork_plan<<<1, kPlan, 0, st>>>(from, to, w, parents, keep ? 1 : 0, status);
+  if (n) k_fork_take<<<n, kBlock, 0, st>>>(from, w);
+  k_fork_rows<<<(unsigned)(to.batch + from.batch), kBlock, 0, st>>>(from, to, w, keep ? 1 : 0);
+  if (tails) k_fork_tails<<<(unsigned)tails, kBlock, 0, st>>>(from, to, w, pools, pieces);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_free(const PagesParams &p, const int32_t *rows, int64_t n, hipStream_t st) {
+  if (n > 0) k_pages_free<<<(unsigned)n, kBlock, 0, st>>>(p, rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const Pools &pools, int64_t n_pages, const int32_t *src,
+                             const int32_t *dst, int64_t n, hipStream_t st) {
+  const int pieces = pieces_of(pools);
+  const int64_t grid = n * pieces;
+  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (grid > 0) k_pages_copy<<<(unsigned)grid, kBlock, 0, st>>>(pools, n_pages, src, dst, pieces);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_t *remap,
+                                int32_t *n_live, char *work, hipStream_t st) {
+  PageWork w;
+  carve_pages(p.n_pages, p.batch, work, &w);
+  const int64_t n = stretches(p.n_pages);
+  const int pieces = pieces_of(pools);
+  if (n) k_pages_count<true><<<(unsigned)n, kBlock, 0, st>>>(p, w);
+  k_compact_plan<<<1, kPlan, 0, st>>>(p, w, n_live);
+  if (n) k_compact_lists<<<(unsigned)n, kBlock, 0, st>>>(p, w, remap);
+  const int counters = (int)(n < 64 ? n : 64);
+  const int64_t movers = std::min<int64_t>((int64_t)p.n_pages / 2 * pieces, 2048);
+  k_compact_move<<<(unsigned)(p.batch + counters + movers), kBlock, 0, st>>>(p, w, pools, remap,
+                                                                            pieces, counters);
+  return hipGetLastError();
+}
+
+}  // namespace sd

@@ -13,6 +13,15 @@ names follow the C ABI in include/sparse_decode.h:
     sparse_decode_dense_attention(q, cache, seq_lens)        -> out
     sparse_decode_label_attention(q, cache, labels, seq_lens, sparsity) -> (out, idx)
     sparse_decode_label_score(q, cache, labels, seq_lens, sparsity)     -> scores
+    sparse_decode_window_attention(q, cache, seq_lens, window, q_starts) -> out
+    sparse_decode_q4_append(k, v, cache4, seq_lens, starts)
+    sparse_decode_q4_load(cache4, seq_lens, starts, tokens)  -> (k, v)
+    sparse_decode_q4_attention(q, cache4, seq_lens, window)  -> out
+    sparse_decode_pages_extend(pages, grow)                  -> status
+    sparse_decode_pages_fork(pages, to, parents, pools)      -> status
+    sparse_decode_pages_free(pages, rows)
+    sparse_decode_pages_copy(pools, src, dst)
+    sparse_decode_pages_compact(pages, pools)                -> (remap, n_live)
 
 Importing this module raises if the library has not been built; nothing here
 falls back to another implementation.
@@ -23,7 +32,7 @@ import ctypes as C
 import dataclasses
 import os
 import struct
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
@@ -32,7 +41,7 @@ LIB_PATH = os.path.join(_HERE, "libsparse_decode.so")
 HEADER_PATH = os.path.join(os.path.dirname(_HERE), "include", "sparse_decode.h")
 
 SD_OK, SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED, SD_ERR_WORKSPACE, SD_ERR_HIP = 0, -1, -2, -3, -4
-SD_F32, SD_BF16, SD_I32 = 0, 1, 2
+SD_F32, SD_BF16, SD_I32, SD_U8 = 0, 1, 2, 3
 SD_KV_BHND, SD_KV_PAGED_NHD = 0, 1
 
 if not os.path.exists(LIB_PATH):
@@ -59,6 +68,21 @@ class SdSparsity(C.Structure):
 
 class SdLabels(C.Structure):
     _fields_ = [("t", SdTensor), ("channels", C.c_void_p)]
+
+
+class SdWindow(C.Structure):
+    _fields_ = [("n_sink", C.c_int32), ("window", C.c_int32), ("softmax_scale", C.c_float)]
+
+
+class SdKv4(C.Structure):
+    _fields_ = [("codes", SdTensor), ("scales", SdTensor), ("layout", C.c_int32),
+                ("page_size", C.c_int32), ("block_table", C.c_void_p),
+                ("max_pages_per_seq", C.c_int32)]
+
+
+class SdPages(C.Structure):
+    _fields_ = [("block_table", C.c_void_p), ("seq_lens", C.c_void_p), ("refs", C.c_void_p),
+                ("n_pages", C.c_int64), ("batch", C.c_int32), ("max_pages", C.c_int32)]
 
 
 class SdProfile(C.Structure):
@@ -120,6 +144,28 @@ lib.sparse_decode_sampled_attention.restype = C.c_int
 lib.sparse_decode_sampled_attention.argtypes = [_P(SdTensor), _P(SdKv), _P(SdKv), C.c_void_p,
                                                 _P(SdSparsity), _P(SdTensor), _P(SdTensor),
                                                 _P(SdTensor), _P(SdTensor), C.c_void_p]
+for _name, _args in {
+        "window_attention": [_P(SdTensor), _P(SdKv), _P(SdKv), C.c_void_p, C.c_void_p, C.c_int64,
+                             _P(SdWindow), _P(SdTensor), C.c_void_p],
+        "window_workspace_size": [_P(SdTensor), _P(SdKv), C.c_int64, C.c_int32, _P(SdWindow),
+                                  _P(C.c_size_t)],
+        "q4_append": [_P(SdTensor), _P(SdTensor), _P(SdKv4), _P(SdKv4), C.c_void_p, C.c_void_p,
+                      C.c_int64, C.c_void_p],
+        "q4_load": [_P(SdKv4), _P(SdKv4), C.c_void_p, C.c_void_p, C.c_int64, _P(SdTensor),
+                    _P(SdTensor), C.c_void_p],
+        "q4_attention": [_P(SdTensor), _P(SdKv4), _P(SdKv4), C.c_void_p, _P(SdWindow),
+                         _P(SdTensor), C.c_void_p],
+        "q4_workspace_size": [_P(SdTensor), _P(SdKv4), _P(SdWindow), _P(C.c_size_t)],
+        "pages_extend": [_P(SdPages), C.c_void_p, C.c_void_p, C.c_void_p],
+        "pages_fork": [_P(SdPages), _P(SdPages), C.c_void_p, C.c_int32, _P(SdTensor), C.c_int32,
+                       C.c_void_p, C.c_void_p],
+        "pages_free": [_P(SdPages), C.c_void_p, C.c_int64, C.c_void_p],
+        "pages_copy": [_P(SdTensor), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p],
+        "pages_compact": [_P(SdPages), _P(SdTensor), C.c_int32, C.c_void_p, C.c_void_p,
+                          C.c_void_p],
+        "pages_workspace_size": [C.c_int64, C.c_int64, _P(C.c_size_t)]}.items():
+    getattr(lib, f"sparse_decode_{_name}").restype = C.c_int
+    getattr(lib, f"sparse_decode_{_name}").argtypes = _args
 lib.sparse_decode_read_probe.restype = C.c_int
 lib.sparse_decode_read_probe.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
 lib.sparse_decode_status_string.restype = C.c_char_p
@@ -130,10 +176,14 @@ lib.sparse_decode_status_string.argtypes = [C.c_int]
 _raw = C.CDLL(LIB_PATH)
 for _name in ("score", "topk", "attend", "attend_weighted", "dense_attention",
               "dense_workspace_size", "label_attention", "label_score", "attention",
-              "attention_noalloc", "workspace_size", "budget", "sampled_attention"):
+              "attention_noalloc", "workspace_size", "budget", "sampled_attention",
+              "window_attention", "window_workspace_size", "q4_append", "q4_load", "q4_attention",
+              "q4_workspace_size", "pages_extend", "pages_fork", "pages_free", "pages_copy",
+              "pages_compact"):
     _f, _g = getattr(lib, f"sparse_decode_{_name}"), getattr(_raw, f"sparse_decode_{_name}")
     _g.restype = _f.restype
-    _g.argtypes = [C.c_void_p if _t in (_P(SdTensor), _P(SdKv), _P(SdSparsity), _P(SdLabels)) else _t
+    _g.argtypes = [C.c_void_p if _t in (_P(SdTensor), _P(SdKv), _P(SdSparsity), _P(SdLabels),
+                                        _P(SdWindow), _P(SdKv4), _P(SdPages)) else _t
                    for _t in _f.argtypes]
 
 
@@ -260,19 +310,23 @@ _PACK_TENSOR = struct.Struct("@Pii4q")
 _PACK_KV = struct.Struct("@Pii4qiIPi4x")
 _PACK_SPARSITY = struct.Struct("@dIIfPII")
 _PACK_LABELS = struct.Struct("@Pii4qP")
+_PACK_WINDOW = struct.Struct("@iif")
+_PACK_KV4 = struct.Struct("@Pii4qPii4qiIPi4x")
+_PACK_PAGES = struct.Struct("@PPPqii")
 for _s, _t in ((_PACK_TENSOR, SdTensor), (_PACK_KV, SdKv), (_PACK_SPARSITY, SdSparsity),
-               (_PACK_LABELS, SdLabels)):
+               (_PACK_LABELS, SdLabels), (_PACK_WINDOW, SdWindow), (_PACK_KV4, SdKv4),
+               (_PACK_PAGES, SdPages)):
     if _s.size != C.sizeof(_t):
         raise ImportError(f"descriptor layout of {_t.__name__} does not match")
 _U32 = 0xFFFFFFFF  # int32 fields wrap, as a ctypes structure's do
 _PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())
 
 
-def _fields(t: torch.Tensor, name: str) -> tuple:
+def _fields(t: torch.Tensor, name: str, dtypes=_DTYPES) -> tuple:
     """The sd_tensor fields of t, in order (the checks of _tensor)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
         _need_device(t, name)  # raises
-    dtype = _DTYPES.get(t.dtype)
+    dtype = dtypes.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{name}: unsupported dtype {t.dtype}")
     shape = t.shape
@@ -564,6 +618,323 @@ def sparse_decode_sampled_attention(q, cache: KVCache, seq_lens, sparsity: Spars
                                                 _stream(stream)),
            "sparse_decode_sampled_attention")
     return out, idx, weights
+
+
+# ---------------------------------------------------------------------------
+# Window attention, the 4-bit cache, and the pages of a paged cache.
+# ---------------------------------------------------------------------------
+@dataclasses.dataclass
+class Window:
+    """What a query at position p sees: the positions j <= p with j < n_sink
+    or p - j < window.  window = EVERYTHING: all of them."""
+    n_sink: int = 0
+    window: int = 2**31 - 1
+    softmax_scale: float = 0.0          # <= 0: 1/sqrt(128)
+
+
+EVERYTHING = 2**31 - 1
+
+
+@dataclasses.dataclass
+class Q4Cache:
+    """Keys and values in 4 bits: codes "bhnd" [B, Hkv, Ncap, 64] with scales
+    [B, Hkv, Ncap, 4], or "paged" [pages, Hkv, 16, 64] with [pages, Hkv, 16, 4]
+    (uint8 all) and an int32 block table [B, max_pages]."""
+    k: torch.Tensor
+    k_scales: torch.Tensor
+    v: torch.Tensor
+    v_scales: torch.Tensor
+    layout: str = "bhnd"
+    block_table: Optional[torch.Tensor] = None
+    page_size: int = 16
+
+    @classmethod
+    def empty(cls, batch: int, kv_heads: int, capacity: int, device="cuda") -> "Q4Cache":
+        """A contiguous cache of empty rows."""
+        return cls(*cls._rows((batch, kv_heads, capacity), device))
+
+    @classmethod
+    def empty_paged(cls, pages: int, kv_heads: int, block_table: torch.Tensor,
+                    device="cuda") -> "Q4Cache":
+        """A pool of empty pages behind a block table."""
+        return cls(*cls._rows((pages, kv_heads, 16), device), layout="paged",
+                   block_table=block_table)
+
+    @staticmethod
+    def _rows(shape, device):
+        return [torch.zeros(shape + (n,), dtype=torch.uint8, device=device) for n in (64, 4, 64, 4)]
+
+    @property
+    def pools(self) -> tuple:
+        """The tensors whose first dimension counts pages (paged layout)."""
+        return self.k, self.k_scales, self.v, self.v_scales
+
+    @property
+    def num_kv_heads(self) -> int:
+        return int(self.k.shape[1])
+
+
+@dataclasses.dataclass
+class Pages:
+    """The pages of a paged cache: sequence b holds the pages
+    block_table[b, :ceil(seq_lens[b] / 16)] (the other entries are -1), refs[p]
+    counts the rows that hold page p (0: free).  int32, changed in place."""
+    block_table: torch.Tensor           # [B, max_pages]
+    seq_lens: torch.Tensor              # [B]
+    refs: torch.Tensor                  # [pages]
+
+
+_DTYPES_U8 = {**_DTYPES, torch.uint8: SD_U8}
+
+
+def _window_desc(w: Window) -> bytes:
+    return _PACK_WINDOW.pack(_int32(w.n_sink, "n_sink"), _int32(w.window, "window"),
+                             C.c_float(w.softmax_scale).value)
+
+
+def _int32(x, name: str) -> int:
+    x = int(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name} must fit in 32 bits")
+    return x
+
+
+def _q4_descs(cache: Q4Cache) -> tuple:
+    if cache.layout == "paged":
+        bt = cache.block_table
+        _need_device(bt, "block_table", torch.int32)
+        tail = (SD_KV_PAGED_NHD, cache.page_size & _U32, bt.data_ptr(), bt.shape[1])
+    elif cache.layout == "bhnd":
+        tail = (SD_KV_BHND, 0, 0, 0)
+    else:
+        raise ValueError(f"unknown layout {cache.layout!r}")
+    return tuple(_PACK_KV4.pack(*_fields(codes, name, _DTYPES_U8),
+                                *_fields(scales, name + "_scales", _DTYPES_U8), *tail)
+                 for name, codes, scales in (("k", cache.k, cache.k_scales),
+                                             ("v", cache.v, cache.v_scales)))
+
+
+def _need_vector(t: torch.Tensor, name: str, n: Optional[int] = None) -> None:
+    _need_device(t, name, torch.int32)
+    if t.dim() != 1 or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must have the shape [{'n' if n is None else n}]")
+
+
+def _batch_of(cache, seq_lens, starts) -> int:
+    """Sequences of a call; checks seq_lens, starts and the block table."""
+    _need_vector(seq_lens, "seq_lens")
+    batch = int(seq_lens.shape[0])
+    if starts is not None:
+        _need_vector(starts, "starts", batch + 1)
+    if cache.layout == "paged" and (cache.block_table is None or cache.block_table.dim() != 2 or
+                                    cache.block_table.shape[0] != batch):
+        raise ValueError(f"block_table must have the shape [{batch}, max_pages]")
+    return batch
+
+
+def _same_device(first: torch.Tensor, *others) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+def _call(fn: str, device, stream, *args) -> None:
+    """One library call on `device`, with the stream appended."""
+    if device.index == torch._C._cuda_getDevice():
+        status = getattr(_raw, fn)(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            status = getattr(_raw, fn)(*args, _stream(stream))
+    _check(status, fn)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """An output, from the memory of the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def sparse_decode_window_attention(q, cache: KVCache, seq_lens, window: Window, q_starts=None,
+                                   out=None, stream=None):
+    """Attention over the positions that `window` leaves visible: one query
+    per sequence (q [B, Hq, 128], at the sequence's last position), or with
+    q_starts (int32 [B + 1]) sequence b's last positions as the rows
+    q_starts[b] .. q_starts[b + 1] of q [T, Hq, 128].  Rows of no sequence
+    are left as they are in `out` (unset without one)."""
+    batch = _batch_of(cache, seq_lens, q_starts)
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    _same_device(q, cache.k, cache.v, cache.block_table, seq_lens, q_starts, out)
+    cq, (kk, kv), co = _desc(q, "q"), _kv_desc(cache, "k", "v"), _desc(out, "out")
+    _call("sparse_decode_window_attention", q.device, stream, cq, kk, kv, seq_lens.data_ptr(),
+          q_starts.data_ptr() if q_starts is not None else None, batch, _window_desc(window), co)
+    return out
+
+
+def window_workspace_size(q, cache: KVCache, seq_lens, window: Window, q_starts=None) -> int:
+    n = C.c_size_t(0)
+    batch = _batch_of(cache, seq_lens, q_starts)
+    cq, kk, cw = _desc(q, "q"), _kv_desc(cache, "k"), _window_desc(window)
+    _check(_raw.sparse_decode_window_workspace_size(cq, kk, batch, int(q_starts is not None), cw,
+                                                    C.byref(n)),
+           "sparse_decode_window_workspace_size")
+    return int(n.value)
+
+
+def sparse_decode_q4_append(k, v, cache: Q4Cache, seq_lens, starts=None, stream=None) -> None:
+    """Write the rows of k and v [T, Hkv, 128] as the last positions of their
+    sequences (seq_lens counts them): row b of sequence b, or with starts
+    (int32 [B + 1]) the rows starts[b] .. starts[b + 1]."""
+    batch = _batch_of(cache, seq_lens, starts)
+    _same_device(k, v, *cache.pools, cache.block_table, seq_lens, starts)
+    ck, cv, (kk, kv) = _desc(k, "k"), _desc(v, "v"), _q4_descs(cache)
+    _call("sparse_decode_q4_append", k.device, stream, ck, cv, kk, kv, seq_lens.data_ptr(),
+          starts.data_ptr() if starts is not None else None, batch)
+
+
+def sparse_decode_q4_load(cache: Q4Cache, seq_lens, starts=None, tokens: Optional[int] = None,
+                          k=None, v=None, dtype=torch.bfloat16, stream=None):
+    """The last positions of each sequence as what their codes stand for: k
+    and v [T, Hkv, 128], rows as in sparse_decode_q4_append (tokens = T, when
+    k and v are not given and starts is).  Rows of no sequence are left as
+    they are (unset in new tensors)."""
+    batch = _batch_of(cache, seq_lens, starts)
+    if (k is None or v is None) and tokens is None:
+        if starts is not None:
+            raise ValueError("tokens: the rows of k and v must be given beside starts")
+        tokens = batch
+    shape = (tokens, cache.num_kv_heads, 128)
+    dev = cache.k.device
+    k = _empty(shape, dtype, dev, stream) if k is None else k
+    v = _empty(shape, dtype, dev, stream) if v is None else v
+    _same_device(k, v, *cache.pools, cache.block_table, seq_lens, starts)
+    ck, cv, (kk, kv) = _desc(k, "k"), _desc(v, "v"), _q4_descs(cache)
+    _call("sparse_decode_q4_load", k.device, stream, kk, kv, seq_lens.data_ptr(),
+          starts.data_ptr() if starts is not None else None, batch, ck, cv)
+    return k, v
+
+
+def sparse_decode_q4_attention(q, cache: Q4Cache, seq_lens, window: Optional[Window] = None,
+                               out=None, stream=None):
+    """Decode attention over a 4-bit cache (bfloat16 q [B, Hq, 128]): every
+    position, or those that `window` leaves visible."""
+    _batch_of(cache, seq_lens, None)
+    if q.shape[0] != seq_lens.shape[0]:
+        raise ValueError("q and seq_lens must have the same number of sequences")
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    _same_device(q, *cache.pools, cache.block_table, seq_lens, out)
+    cq, (kk, kv), co = _desc(q, "q"), _q4_descs(cache), _desc(out, "out")
+    cw = _window_desc(window) if window is not None else None
+    _call("sparse_decode_q4_attention", q.device, stream, cq, kk, kv, seq_lens.data_ptr(), cw, co)
+    return out
+
+
+def q4_workspace_size(q, cache: Q4Cache, window: Optional[Window] = None) -> int:
+    n = C.c_size_t(0)
+    cq, (kk, _) = _desc(q, "q"), _q4_descs(cache)
+    cw = _window_desc(window) if window is not None else None
+    _check(_raw.sparse_decode_q4_workspace_size(cq, kk, cw, C.byref(n)),
+           "sparse_decode_q4_workspace_size")
+    return int(n.value)
+
+
+def _pages_desc(pages: Pages) -> bytes:
+    bt = pages.block_table
+    _need_device(bt, "block_table", torch.int32)
+    if bt.dim() != 2:
+        raise ValueError("block_table must have the shape [batch, max_pages]")
+    _need_vector(pages.seq_lens, "seq_lens", int(bt.shape[0]))
+    _need_vector(pages.refs, "refs")
+    _same_device(bt, pages.seq_lens, pages.refs)
+    return _PACK_PAGES.pack(bt.data_ptr(), pages.seq_lens.data_ptr(), pages.refs.data_ptr(),
+                            pages.refs.shape[0], bt.shape[0], bt.shape[1])
+
+
+def _pools_desc(pools: Sequence[torch.Tensor], device) -> tuple:
+    for t in pools:
+        if t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device}")
+    return b"".join(_PACK_TENSOR.pack(*_fields(t, "pools", _DTYPES_U8)) for t in pools), len(pools)
+
+
+def sparse_decode_pages_extend(pages: Pages, grow, status=None, stream=None):
+    """Pages for grow[b] more positions of each row (int32 [B]), the lowest
+    free ones first; seq_lens grows.  Returns status int32 [B]: 0 done, 1 no
+    free pages left, 2 longer than the table; such rows stay as they are."""
+    cp, batch, dev = _pages_desc(pages), int(pages.block_table.shape[0]), pages.block_table.device
+    _need_vector(grow, "grow", batch)
+    status = _empty((batch,), torch.int32, dev, stream) if status is None else status
+    _need_vector(status, "status", batch)
+    _same_device(pages.block_table, grow, status)
+    _call("sparse_decode_pages_extend", dev, stream, cp, grow.data_ptr(), status.data_ptr())
+    return status
+
+
+def sparse_decode_pages_fork(pages: Pages, to: Pages, parents, pools: Sequence[torch.Tensor] = (),
+                             keep: bool = True, status=None, stream=None):
+    """Row i of `to` becomes a child of row parents[i] of `pages` (int32;
+    outside its rows: an empty row): full pages are shared, a part-filled last
+    page is copied in every pool.  keep=False ends the parents' rows (a step
+    of beam search).  Returns status int32: 0 done, 1 no free page left."""
+    cp, ct, dev = _pages_desc(pages), _pages_desc(to), pages.block_table.device
+    batch = int(to.block_table.shape[0])
+    _need_vector(parents, "parents", batch)
+    status = _empty((batch,), torch.int32, dev, stream) if status is None else status
+    _need_vector(status, "status", batch)
+    _same_device(pages.block_table, to.block_table, parents, status)
+    pl, n = _pools_desc(pools, dev)
+    _call("sparse_decode_pages_fork", dev, stream, cp, ct, parents.data_ptr(), int(bool(keep)), pl,
+          n, status.data_ptr())
+    return status
+
+
+def sparse_decode_pages_free(pages: Pages, rows, stream=None) -> None:
+    """The listed rows (int32) give back their pages and are left empty."""
+    cp = _pages_desc(pages)
+    _need_vector(rows, "rows")
+    _same_device(pages.block_table, rows)
+    _call("sparse_decode_pages_free", rows.device, stream, cp, rows.data_ptr(), rows.shape[0])
+
+
+def sparse_decode_pages_copy(pools: Sequence[torch.Tensor], src, dst, stream=None) -> None:
+    """Page dst[i] = page src[i] in every pool (int32; a page is not both a
+    source and a destination, nor a destination twice)."""
+    _need_vector(src, "src")
+    _need_vector(dst, "dst", int(src.shape[0]))
+    _same_device(src, dst)
+    pl, n = _pools_desc(pools, src.device)
+    _call("sparse_decode_pages_copy", src.device, stream, pl, n, src.data_ptr(), dst.data_ptr(),
+          src.shape[0])
+
+
+def sparse_decode_pages_compact(pages: Pages, pools: Sequence[torch.Tensor] = (), remap=None,
+                                n_live=None, stream=None):
+    """Move the live pages to the front of the pools; table and refs follow.
+    Returns (remap int32 [pages]: where each page is now, -1 if it was free;
+    n_live int32 [1])."""
+    cp, dev = _pages_desc(pages), pages.block_table.device
+    n = int(pages.refs.shape[0])
+    remap = _empty((n,), torch.int32, dev, stream) if remap is None else remap
+    n_live = _empty((1,), torch.int32, dev, stream) if n_live is None else n_live
+    _need_vector(remap, "remap", n)
+    _need_vector(n_live, "n_live", 1)
+    _same_device(pages.block_table, remap, n_live)
+    pl, count = _pools_desc(pools, dev)
+    _call("sparse_decode_pages_compact", dev, stream, cp, pl, count, remap.data_ptr(),
+          n_live.data_ptr())
+    return remap, n_live
+
+
+def pages_workspace_size(n_pages: int, batch: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib.sparse_decode_pages_workspace_size(int(n_pages), int(batch), C.byref(n)),
+           "sparse_decode_pages_workspace_size")
+    return int(n.value)
 
 
 def read_probe(buf: torch.Tensor, sink: torch.Tensor, stream=None) -> None:
