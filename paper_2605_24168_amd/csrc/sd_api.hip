@@ -1243,9 +1243,13 @@ sd::WindowParams window_params(const CacheShape &c, int64_t batch, int64_t rows,
   return p;
 }
 
-size_t token_work_bytes(const sd::WindowParams &p) {
+// Splits of a call (one query per sequence, or packed ones) and the bytes of
+// its partials.
+size_t window_work(sd::WindowParams &p, int kind, bool packed) {
+  if (packed) sd::chunk_split(p, kind);
+  else sd::window_split(p, kind);
   if (p.nsplit <= 1) return 0;
-  return align_up((size_t)p.batch * p.hq * p.nsplit * sd::kPartStride * sizeof(float));
+  return align_up((size_t)p.n_rows * p.hq * p.nsplit * sd::kPartStride * sizeof(float));
 }
 
 // The checks that window attention and its workspace size share.
@@ -1266,20 +1270,20 @@ sd_status check_window_call(const sd_tensor *q, const sd_kv *K, int64_t batch, b
   return SD_OK;
 }
 
-// Splits and scratch of a decode call (one query per sequence).
-sd_status run_token(sd::WindowParams &p, int kind, bool paged, void *stream) {
+// Splits, scratch and launches of a call.
+sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
+  const bool packed = p.q_starts != nullptr;
+  const size_t bytes = window_work(p, kind, packed);
   std::lock_guard<std::mutex> lk(g_mu);
-  DevState *ds = nullptr;
-  sd_status st = device_state(ds);
-  if (st) return st;
-  sd::window_split(p, kind);
-  if (p.nsplit > 1) {
+  if (bytes) {
+    DevState *ds = nullptr;
     char *base = nullptr;
-    st = get_workspace(token_work_bytes(p), ds, base);
+    const sd_status st = get_workspace(bytes, ds, base);
     if (st) return st;
     p.part = (float *)base;
   }
-  return hip_status(sd::launch_token_attend(p, kind, paged, (hipStream_t)stream));
+  return hip_status(packed ? sd::launch_chunk_attend(p, kind, paged, (hipStream_t)stream)
+                           : sd::launch_token_attend(p, kind, paged, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -1293,11 +1297,8 @@ sd_status sparse_decode_window_workspace_size(const sd_tensor *q, const sd_kv *K
   int64_t rows = 0, hq = 0;
   const sd_status st = check_window_call(q, K, batch, packed != 0, w, c, rows, hq);
   if (st) return st;
-  *bytes = 0;
-  if (packed) return SD_OK;
   sd::WindowParams p = window_params(c, batch, rows, hq, w);
-  sd::window_split(p, q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16);
-  *bytes = token_work_bytes(p);
+  *bytes = window_work(p, q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16, packed != 0);
   return SD_OK;
 }
 
@@ -1328,8 +1329,7 @@ sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, con
   p.seq_lens = seq_lens;
   p.q_starts = q_starts;
   const int kind = q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16;
-  if (!q_starts) return run_token(p, kind, c.paged, stream);
-  return hip_status(sd::launch_chunk_attend(p, kind, c.paged, (hipStream_t)stream));
+  return run_window(p, kind, c.paged, stream);
 }
 
 sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K, const sd_window *w,
@@ -1346,8 +1346,7 @@ sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K, c
   if (hq % c.hkv) return SD_ERR_INVALID_ARG;
   if (hq / c.hkv > sd::kMaxGroup) return SD_ERR_UNSUPPORTED;
   sd::WindowParams p = window_params(c, rows, rows, hq, w);
-  sd::window_split(p, sd::kCacheQ4);
-  *bytes = token_work_bytes(p);
+  *bytes = window_work(p, sd::kCacheQ4, false);
   return SD_OK;
 }
 
@@ -1376,7 +1375,7 @@ sd_status sparse_decode_q4_attention(const sd_tensor *q, const sd_kv4 *K, const 
   p.vs = (const uint8_t *)V->scales.data;
   p.block_table = K->block_table;
   p.seq_lens = seq_lens;
-  return run_token(p, sd::kCacheQ4, c.paged, stream);
+  return run_window(p, sd::kCacheQ4, c.paged, stream);
 }
 
 }  // extern "C"

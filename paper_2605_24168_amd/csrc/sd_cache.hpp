@@ -26,7 +26,8 @@ struct WindowParams {
   const int32_t *block_table;  // paged: [batch, max_pages]
   const int32_t *seq_lens;     // [batch]
   const int32_t *q_starts;     // [batch + 1]; null: one query per sequence
-  float *part;                 // [T * Hq][nsplit][kPartStride], see k_token_merge
+  float *part;                 // [T * Hq][nsplit][kPartStride]: maximum in powers of two,
+                               // sum, 128 unnormalised channels of a split
   int64_t ncap;                // positions addressable per sequence
   int64_t n_rows;              // T
   int32_t n_pages;             // pages of the pool
@@ -41,6 +42,8 @@ struct WindowParams {
 // Splits of one sequence and KV head over workgroups, from what the host
 // knows (see window_split); fills p.span and p.nsplit.
 void window_split(WindowParams &p, int kind);
+// The same for packed queries; fills p.nsplit.
+void chunk_split(WindowParams &p, int kind);
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 
@@ -80,6 +83,56 @@ hipError_t launch_pages_copy(const Pools &pools, int64_t n_pages, const int32_t 
                              const int32_t *dst, int64_t n, hipStream_t st);
 hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_t *remap,
                                 int32_t *n_live, char *work, hipStream_t st);
+
+// Two floats rounded to bfloat16 (to nearest even), the first in the low half.
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, b16x2));
+}
+
+// A row's partials joined by one wave: lane l gets channels 2l and 2l + 1 of
+// the n splits at pp, divided by their sum.  Each lane takes a split's maximum
+// and sum, so that their loads are under way together.
+struct Joined {
+  float x, y;
+};
+__device__ __forceinline__ Joined join_splits(const float *pp, int n) {
+  const int l = lane_id();
+  float m = -3e38f;
+  for (int s = l; s < n; s += 64) m = fmaxf(m, pp[(int64_t)s * kPartStride]);
+  const float M = wave_max(m);
+  float sum = 0.f, x = 0.f, y = 0.f;
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    const int s = s0 + l;
+    float f = 0.f;
+    if (s < n) {
+      f = __builtin_amdgcn_exp2f(pp[(int64_t)s * kPartStride] - M);
+      sum += f * pp[(int64_t)s * kPartStride + 1];
+    }
+    const int k = n - s0 < 64 ? n - s0 : 64;
+    const float *o = pp + (int64_t)s0 * kPartStride + 2 + 2 * l;
+    for (int i0 = 0; i0 < k; i0 += 8) {  // eight loads under way together
+      float2 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t j = i0 + i < k ? i0 + i : k - 1;
+        v[i] = float2{o[j * kPartStride], o[j * kPartStride + 1]};
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float fi =
+            i0 + i < k ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (i0 + i) & 63)) : 0.f;
+        x = fmaf(fi, v[i].x, x);
+        y = fmaf(fi, v[i].y, y);
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  return Joined{x * inv, y * inv};
+}
 
 // Sequence length, clamped to the capacity.
 __device__ __forceinline__ int clamp_len(const int32_t *seq_lens, int b, int64_t ncap) {

@@ -18,6 +18,8 @@
 // transposing LDS reads (bfloat16) or plain ones (float32).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "sd_cache.hpp"
 #include "sd_internal.hpp"
 
@@ -32,36 +34,36 @@ constexpr float kChunkFloor = -1e30f;
 constexpr float kChunkSlack = 8.f;
 
 // The workgroup's rows: sequence, its first row there, rows of the sequence.
+// (T * Hq rows of q fit in 31 bits, so all of these do.)
 struct ChunkItem {
   int b;
-  int64_t row0;    // of the sequence's n * G rows
-  int64_t rows;    // n * G
-  int64_t start;   // the sequence's first row of q, in tokens
+  int row0;    // of the sequence's n * G rows
+  int rows;    // n * G
+  int start;   // the sequence's first row of q, in tokens
 };
 
-// Item i of the row tiles of all sequences in order; false past the last.
-// Every wave finds it for itself: 64 sequences at a time by a prefix sum.
-__device__ __forceinline__ bool chunk_item(const WindowParams &p, int64_t i, ChunkItem &it) {
-  int64_t before = 0;
+// Item i of the row tiles (ROWS rows) of all sequences in order; false past the
+// last.  Every wave finds it for itself: 64 sequences at a time by a prefix sum.
+template <int ROWS>
+__device__ __forceinline__ bool chunk_item(const WindowParams &p, int i, ChunkItem &it) {
+  int before = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 64) {
     const int b = b0 + lane_id();
-    int64_t s = 0, n = 0;
+    int s = 0, n = 0;
     if (b < p.batch) {
-      s = clamp_start(p.q_starts, b, p.n_rows);
-      n = clamp_start(p.q_starts, b + 1, p.n_rows) - s;
-      n = n < 0 ? 0 : n;
+      s = (int)clamp_start(p.q_starts, b, p.n_rows);
+      n = max(0, (int)clamp_start(p.q_starts, b + 1, p.n_rows) - s);
     }
-    const int mine = (int)((n * p.G + kChunkRows - 1) / kChunkRows);
+    const int mine = (n * p.G + ROWS - 1) / ROWS;
     const int upto = wave_incl_scan(mine);
-    const int64_t end = before + upto;
-    const uint64_t hit = __ballot(i < end);
+    const uint64_t hit = __ballot(i - before < upto);
     if (hit) {
       const int src = __ffsll((unsigned long long)hit) - 1;
       it.b = b0 + src;
-      const int first = __shfl(upto - mine, src);
-      it.row0 = (i - before - first) * kChunkRows;
-      it.start = __shfl((int)s, src);
-      it.rows = (int64_t)__shfl((int)n, src) * p.G;
+      const int first = __builtin_amdgcn_readlane(upto - mine, src);
+      it.row0 = (i - before - first) * ROWS;
+      it.start = __builtin_amdgcn_readlane(s, src);
+      it.rows = __builtin_amdgcn_readlane(n, src) * p.G;
       return true;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
@@ -69,16 +71,6 @@ __device__ __forceinline__ bool chunk_item(const WindowParams &p, int64_t i, Chu
   return false;
 }
 
-template <int KIND>
-struct ChunkLds {
-  static constexpr int kRowBytes = KIND == kCacheF32 ? 512 : 256;
-  u32x4 k[kChunkKeys * kRowBytes / 16];
-  u32x4 v[kChunkKeys * kRowBytes / 16];
-};
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  return (uint32_t)f32_to_bf16_rne(a) | ((uint32_t)f32_to_bf16_rne(b) << 16);
-}
 __device__ __forceinline__ bf16x8 frag(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
 
 // Four rows of one column of 16-bit values: lane i of 16 gives the address of
@@ -88,134 +80,168 @@ __device__ __forceinline__ u32x2 read_columns(const char *lds) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lds));
 }
 
-template <int KIND, bool PAGED>
-__global__ __launch_bounds__(kBlock) void k_chunk_attend(WindowParams p) {
-  constexpr bool F32 = KIND == kCacheF32;
-  constexpr int kRowBytes = ChunkLds<KIND>::kRowBytes;
-  constexpr int kChunks = kRowBytes / 16;            // 16-byte chunks per row
-  constexpr int kLoads = kChunkKeys * kChunks / kBlock;  // per thread and tile
-  constexpr int kRowsPerLoad = kBlock / kChunks;
-  extern __shared__ u32x4 lds_raw[];
-  ChunkLds<KIND> &lds = *(ChunkLds<KIND> *)lds_raw;
-
-  const int g = (int)(blockIdx.x % p.hkv);
-  ChunkItem it;
-  if (!chunk_item(p, blockIdx.x / p.hkv, it)) return;
-  const int b = it.b;
-  const int L = clamp_len(p.seq_lens, b, p.ncap);
-  const int n = (int)(it.rows / p.G);
-  const int l = lane_id(), w = wave_id(), col = l & 31, half = l >> 5;
-
-  // This lane's row: its token's position and where its query is.
-  const int64_t row = it.row0 + 32 * w + col;
-  const bool live = row < it.rows;
-  const int tok = (int)((live ? row : it.rows - 1) / p.G);
-  const int head = g * p.G + (int)((live ? row : it.rows - 1) % p.G);
-  const int pos = L - n + tok;
-  const int64_t qat = ((it.start + tok) * p.hq + head) * kHeadDim;
-
-  // Positions of the workgroup's first and last token.
-  const int64_t rlast = min(it.row0 + kChunkRows, it.rows) - 1;
-  const int pmin = L - n + (int)(it.row0 / p.G), pmax = L - n + (int)(rlast / p.G);
-
-  u32x4 q[F32 ? 16 : 8];
-#pragma unroll
-  for (int i = 0; i < (F32 ? 16 : 8); ++i) {
-    if (F32) q[i] = *(const u32x4 *)((const float *)p.q + qat + 8 * i + 4 * half);
-    else q[i] = *(const u32x4 *)((const uint16_t *)p.q + qat + 16 * i + 8 * half);
+// What the rows [row0, row0 + ROWS) of a sequence see, as tiles of KEYS
+// positions: those of the first tokens, then those of the windows, [t0, t1) of
+// them for this split.
+template <int ROWS, int KEYS>
+struct ChunkRange {
+  int L, n;          // positions, queries of the sequence
+  int pmin, pmax;    // positions of the first and last row
+  int sink, lo;      // some row sees j < sink or j >= lo
+  int na, b0, t0, t1;
+  __device__ __forceinline__ ChunkRange(const WindowParams &p, const ChunkItem &it, int split) {
+    L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, it.b, p.ncap));
+    n = it.rows / p.G;
+    pmin = position(p, it, it.row0);
+    pmax = position(p, it, it.row0 + ROWS - 1);
+    sink = min(p.n_sink, pmax + 1);
+    lo = pmin + 1 > p.window ? pmin + 1 - p.window : 0;
+    na = sink > 0 ? (sink + KEYS - 1) / KEYS : 0;
+    b0 = lo / KEYS;
+    b0 = b0 < na ? na : b0;
+    const int end = p.window > 0 && pmax >= 0 ? pmax / KEYS + 1 : 0;
+    const int nt = na + (end > b0 ? end - b0 : 0);
+    t0 = (int)((int64_t)nt * split / p.nsplit);
+    t1 = (int)((int64_t)nt * (split + 1) / p.nsplit);
   }
+  __device__ __forceinline__ int position(const WindowParams &p, const ChunkItem &it, int row) const {
+    return L - n + (int)((uint32_t)min(row, it.rows - 1) / (uint32_t)p.G);
+  }
+  __device__ __forceinline__ int first_of(int t) const { return (t < na ? t : t - na + b0) * KEYS; }
+};
 
-  f32x16 acc[4];
+// A row's query: where it is in q (and out), and its position.
+struct ChunkRow {
+  bool live;
+  int pos, first;    // first: its visible first tokens
+  int64_t at;        // elements
+  __device__ __forceinline__ ChunkRow(const WindowParams &p, const ChunkItem &it, int row, int g, int L,
+                                      int n) {
+    live = row < it.rows;
+    const uint32_t r = min(row, it.rows - 1);
+    const int tok = (int)(r / (uint32_t)p.G), head = g * p.G + (int)(r % (uint32_t)p.G);
+    pos = L - n + tok;
+    first = min(p.n_sink, pos + 1);
+    at = ((int64_t)(it.start + tok) * p.hq + head) * kHeadDim;
+  }
+};
+
+// (split, KV head, row tile) of a workgroup; false: no such rows.
+template <int ROWS>
+__device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, int &split, ChunkItem &it) {
+  uint32_t i = blockIdx.x;
+  g = (int)(i % (uint32_t)p.hkv);
+  i /= (uint32_t)p.hkv;
+  split = (int)(i % (uint32_t)p.nsplit);
+  return chunk_item<ROWS>(p, (int)(i / (uint32_t)p.nsplit), it);
+}
+
+// ---------------------------------------------------------------------------
+// float32: bound by the matrix unit at a sixteenth of its bfloat16 rate, so
+// operands come straight from global memory.  The four waves of a workgroup
+// share 32 rows and take every fourth tile of 32 positions each; they join at
+// the end.  While the scores of a tile are computed its values are under way,
+// while those are added the next tile's keys.
+// ---------------------------------------------------------------------------
+constexpr int kF32Rows = 32;
+constexpr int kF32Keys = 32;
+
+template <bool PAGED>
+__global__ __launch_bounds__(kBlock, 1) void k_chunk_f32(WindowParams p) {
+  __shared__ float lds_q[kF32Rows * kHeadDim];          // [channel / 4][row][4]
+  __shared__ float lds_o[2][kF32Rows * (kHeadDim + 4)];
+  __shared__ float lds_ml[kWaves][kF32Rows][2];
+  int g, split;
+  ChunkItem it;
+  if (!chunk_place<kF32Rows>(p, g, split, it)) return;
+  const ChunkRange<kF32Rows, kF32Keys> cr(p, it, split);
+  const int l = lane_id(), col = l & 31, half = l >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(wave_id());
+  const ChunkRow row(p, it, it.row0 + col, g, cr.L, cr.n);
+  for (int i = threadIdx.x >> 5; i < 32; i += kBlock / 32)   // thread: row, 16-byte chunk i
+    *(f32x4 *)&lds_q[(i * 32 + col) * 4] = *(const f32x4 *)((const float *)p.q + row.at + 4 * i);
+  __syncthreads();
+
+  f32x16 acc[4];   // acc[c], register r: channel 4 (8 (r / 4) + 4 half + r % 4) + c
+  float m = kChunkFloor, ls = 0.f;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
-  float m = kChunkFloor, ls = 0.f;
 
-  // Tiles: those of the first tokens, then those of the windows.
-  const int sink = min(p.n_sink, pmax + 1);
-  const int lo = pmin + 1 > p.window ? pmin + 1 - p.window : 0;  // first position of a window
-  const int na = sink > 0 ? (sink + kChunkKeys - 1) / kChunkKeys : 0;
-  int b0 = lo / kChunkKeys;
-  b0 = b0 < na ? na : b0;
-  const int end = p.window > 0 && pmax >= 0 ? pmax / kChunkKeys + 1 : 0;
-  const int nt = na + (end > b0 ? end - b0 : 0);
-  const int lrow = threadIdx.x / kChunks, lchunk = threadIdx.x % kChunks;
+  // A tile's 32 positions lie on two pages; bad: bits of positions whose page
+  // is not in the pool.
+  const int step = (PAGED ? p.hkv : 1) * 512;   // bytes from row to row
+  struct Where {
+    int64_t at[2];    // bytes, of the first and second 16 rows
+    uint32_t bad;
+  };
+  auto locate = [&](int j0) {
+    Where x;
+    x.bad = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = j0 + kTile * i;
+      if (!PAGED) {
+        x.at[i] = (((int64_t)it.b * p.hkv + g) * p.ncap + j) * 512;
+        continue;
+      }
+      int page = j <= cr.pmax ? p.block_table[(int64_t)it.b * p.max_pages + (j >> 4)] : 0;
+      if (page < 0 || page >= p.n_pages) {
+        page = 0;
+        x.bad |= 0xFFFFu << (16 * i);
+      }
+      x.at[i] = ((int64_t)page * kTile * p.hkv + g) * 512;
+    }
+    return x;
+  };
+  // Row x of the tile at j0, in bytes.  (A page has all its rows; of a
+  // contiguous cache, only those up to the last position may be read.)
+  auto row_at = [&](const Where &wh, int j0, int x) {
+    const int y = PAGED ? x : min(x, cr.pmax - j0);
+    return PAGED ? wh.at[x >> 4] + (int64_t)((y & 15) * step) : wh.at[0] + (int64_t)(y * step);
+  };
+  f32x4 kf[16], vf[16];
+  Where now, next;
+  auto bring_keys = [&](int j0) {
+    next = locate(j0);
+    const char *src = p.k + row_at(next, j0, col) + 16 * half;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) kf[i] = *(const f32x4 *)(src + 32 * i);
+  };
+  auto bring_values = [&](int j0) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      vf[r] = *(const f32x4 *)(p.v + row_at(now, j0, 8 * (r >> 2) + 4 * half + (r & 3)) + 16 * col);
+  };
 
-  for (int t = 0; t < nt; ++t) {
-    const int j0 = (t < na ? t : t - na + b0) * kChunkKeys;
-    // Stage the tile.  Rows that none of the workgroup's queries sees become
-    // zeros: a weight of 0 times whatever they hold must stay 0.
-    uint64_t gone = 0;  // positions on pages outside the pool, by 16
+  if (cr.t0 + w < cr.t1) bring_keys(cr.first_of(cr.t0 + w));
+  for (int t = cr.t0 + w; t < cr.t1; t += kWaves) {
+    const int j0 = cr.first_of(t);
+    now = next;
+    bring_values(j0);
+    f32x16 sc;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = i * kRowsPerLoad + lrow, j = j0 + r;
-      bool ok = j <= pmax && (j < sink || j >= lo);
-      int64_t at = 0;
-      if (PAGED) {
-        int page = -1;
-        if (j <= pmax) page = p.block_table[(int64_t)b * p.max_pages + (j >> 4)];
-        ok = ok && page >= 0 && page < p.n_pages;
-        at = ((int64_t)page * kTile + (j & 15)) * p.hkv + g;
-      } else {
-        at = ((int64_t)b * p.hkv + g) * p.ncap + j;
-      }
-      u32x4 kv = {0u, 0u, 0u, 0u}, vv = {0u, 0u, 0u, 0u};
-      if (ok) {
-        kv = *(const u32x4 *)(p.k + at * kRowBytes + 16 * lchunk);
-        vv = *(const u32x4 *)(p.v + at * kRowBytes + 16 * lchunk);
-      }
-      if (F32) {
-        lds.k[r * kChunks + (lchunk ^ (r & 15))] = kv;
-        lds.v[r * kChunks + lchunk] = vv;
-      } else {
-        lds.k[r * kChunks + (lchunk ^ (r & 15))] = kv;
-        lds.v[r * kChunks + (lchunk ^ ((r & 3) << 2))] = vv;
-      }
+    for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const f32x4 qf = *(const f32x4 *)&lds_q[((2 * i + half) * 32 + col) * 4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i][e], qf[e], sc, 0, 0, 0);
     }
-    if (PAGED) {  // which of the tile's pages are not in the pool
-#pragma unroll
-      for (int i = 0; i < kChunkKeys / kTile; ++i) {
-        const int j = j0 + kTile * i;
-        int page = -1;
-        if (j <= pmax) page = p.block_table[(int64_t)b * p.max_pages + (j >> 4)];
-        if (page < 0 || page >= p.n_pages) gone |= 1ull << i;
-      }
-    }
-    __syncthreads();
-
-    f32x16 sc[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[x][r] = 0.f;
-      const int kr = 32 * x + col;
-#pragma unroll
-      for (int i = 0; i < (F32 ? 16 : 8); ++i) {
-        const u32x4 kf = lds.k[kr * kChunks + ((2 * i + half) ^ (kr & 15))];
-        if constexpr (F32) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t kw = kf[e], qw = q[i][e];
-            sc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kw), __uint_as_float(qw),
-                                                         sc[x], 0, 0, 0);
-          }
-        } else {
-          sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(kf), frag(q[i]), sc[x], 0, 0, 0);
-        }
-      }
-    }
+    if (t + kWaves < cr.t1) bring_keys(cr.first_of(t + kWaves));
     float top = -__builtin_inff();
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = j0 + 32 * x + 8 * (r >> 2) + 4 * half + (r & 3);
-        const bool sees = j <= pos && (j < p.n_sink || pos - j < p.window) &&
-                          !(gone >> (2 * x + (r >> 3)) & 1);
-        sc[x][r] = sees ? sc[x][r] : -__builtin_inff();
-        top = fmaxf(top, sc[x][r]);
-      }
+    for (int r = 0; r < 16; ++r) {
+      const int x = 8 * (r >> 2) + 4 * half + (r & 3), j = j0 + x;
+      const bool sees = (j < row.first) | ((uint32_t)(row.pos - j) < (uint32_t)p.window);
+      const bool there = !(now.bad >> x & 1);
+      sc[r] = (sees & there) ? sc[r] : -__builtin_inff();
+      top = fmaxf(top, sc[r]);
+      // A position that no row sees weighs 0, whatever its values hold.
+      if (!there || j > cr.pmax || (j >= cr.sink && j < cr.lo)) vf[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     if (__ballot(top * p.scale2 > m + kChunkSlack)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float mn = fmaxf(m, top * p.scale2);
@@ -226,79 +252,363 @@ __global__ __launch_bounds__(kBlock) void k_chunk_attend(WindowParams p) {
       for (int c = 0; c < 4; ++c) acc[c] *= f;
     }
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int r = 0; r < 16; ++r) {
+      sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], p.scale2, -m));
+      ls += sc[r];
+    }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[x][r] = __builtin_amdgcn_exp2f(fmaf(sc[x][r], p.scale2, -m));
-        ls += sc[x][r];
-      }
-    // O^T += V^T p^T.
-    if constexpr (F32) {
-      const float *v = (const float *)lds.v;
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int c = 0; c < 4; ++c)
+        acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][c], sc[r], acc[c], 0, 0, 0);
+  }
+
+  // Join the waves: to the common maximum, then pairwise sums of outputs.
+  ls += __shfl_xor(ls, 32);
+  if (half == 0) {
+    lds_ml[w][col][0] = m;
+    lds_ml[w][col][1] = ls;
+  }
+  __syncthreads();
+  float M = kChunkFloor, sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int vr = 32 * x + 8 * (r >> 2) + 4 * half + (r & 3);
+  for (int x = 0; x < kWaves; ++x) M = fmaxf(M, lds_ml[x][col][0]);
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[vr * kHeadDim + 32 * c + col], sc[x][r],
-                                                          acc[c], 0, 0, 0);
-        }
+  for (int x = 0; x < kWaves; ++x)
+    sum += __builtin_amdgcn_exp2f(lds_ml[x][col][0] - M) * lds_ml[x][col][1];
+  const float f = __builtin_amdgcn_exp2f(m - M);
+  auto each = [&](auto op) {   // op(float4 at channels .., values of this wave)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int c = 4 * (8 * (r >> 2) + 4 * half + (r & 3));
+      op(c, f32x4{acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
+    }
+  };
+#pragma unroll
+  for (int c = 0; c < 4; ++c) acc[c] *= f;
+  float *mine = &lds_o[w & 1][col * (kHeadDim + 4)];
+  if (w >= 2) each([&](int c, f32x4 x) { *(f32x4 *)(mine + c) = x; });
+  __syncthreads();
+  if (w < 2) each([&](int c, f32x4 x) { *(f32x4 *)(mine + c) = x + *(f32x4 *)(mine + c); });
+  __syncthreads();
+  if (!row.live) return;
+  const int64_t orow = row.at / kHeadDim;
+  float *pp = p.part + (orow * p.nsplit + split) * kPartStride;
+  if (p.nsplit > 1 && threadIdx.x < 32) {
+    pp[0] = M;
+    pp[1] = sum;
+  }
+  const float inv = p.nsplit > 1 ? 1.f : (sum > 0.f ? 1.f / sum : 0.f);
+  for (int i = threadIdx.x >> 5; i < 32; i += kBlock / 32) {
+    const int c = 4 * i, at = col * (kHeadDim + 4) + c;
+    const f32x4 x = (*(f32x4 *)&lds_o[0][at] + *(f32x4 *)&lds_o[1][at]) * inv;
+    if (p.nsplit == 1) {
+      *(f32x4 *)((float *)p.out + row.at + c) = x;
     } else {
-      // (weights round to bfloat16, as the values are: half a step, 2^-9)
-      const int i16 = l & 15, c16 = (l >> 4) & 1;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const f32x16 &ss = sc[s >> 1];
-        const int r0 = 8 * (s & 1);
-        const u32x4 pw = {pack2(ss[r0], ss[r0 + 1]), pack2(ss[r0 + 2], ss[r0 + 3]),
-                          pack2(ss[r0 + 4], ss[r0 + 5]), pack2(ss[r0 + 6], ss[r0 + 7])};
-        const int vr = 16 * s + 4 * half + (i16 >> 2);
+      for (int e = 0; e < 4; ++e) pp[2 + c + e] = x[e];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// bfloat16: the tiles go from memory straight into LDS, and a wave computes
+// the scores of one tile while it turns those of the tile before into weights,
+// so that the matrix unit and the vector unit have work at the same time.
+// ---------------------------------------------------------------------------
+struct ChunkStage {
+  u32x4 k[2][kChunkKeys * 16];   // tiles of keys and values, by parity
+  u32x4 v[2][kChunkKeys * 16];
+};
+
+// Rows that are not to be read come from here.
+__device__ const u32x4 chunk_zeros[16] = {};
+
+template <bool PAGED>
+__global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
+  extern __shared__ u32x4 lds_raw[];
+  ChunkStage &lds = *(ChunkStage *)lds_raw;
+  int g, split;
+  ChunkItem it;
+  if (!chunk_place<kChunkRows>(p, g, split, it)) return;
+  const ChunkRange<kChunkRows, kChunkKeys> cr(p, it, split);
+  const int b = it.b;
+  const int l = lane_id(), col = l & 31, half = l >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(wave_id());
+  const ChunkRow row(p, it, it.row0 + 32 * w + col, g, cr.L, cr.n);
+  u32x4 q[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int chunk = 4 * c + 2 * c16 + ((i16 & 3) >> 1);
-          const char *base = (const char *)lds.v + 16 * (chunk ^ ((vr & 3) << 2)) + 8 * (i16 & 1);
-          const u32x2 x = read_columns(base + vr * 256), y = read_columns(base + (vr + 8) * 256);
-          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(u32x4{x[0], x[1], y[0], y[1]}),
-                                                           frag(pw), acc[c], 0, 0, 0);
-        }
+  for (int i = 0; i < 8; ++i) q[i] = *(const u32x4 *)((const uint16_t *)p.q + row.at + 16 * i + 8 * half);
+
+  const int wmin = cr.position(p, it, it.row0 + 32 * w);
+  const int wmax = cr.position(p, it, it.row0 + 32 * w + 31);
+
+  // Pages of 16 tiles at a time, one per lane, from tile `held` on; outside: a
+  // bit for each that is not in the pool.
+  int pages = 0, held = -16;
+  uint64_t outside = 0;
+  auto hold_pages = [&](int t) {
+    if (!PAGED || t < held + 16) return;
+    held = t;
+    const int j = cr.first_of(t + (l >> 2)) + kTile * (l & 3);
+    pages = 0;
+    bool ok = true;
+    if (t + (l >> 2) < cr.t1 && j <= cr.pmax) {
+      pages = p.block_table[(int64_t)b * p.max_pages + (j >> 4)];
+      ok = pages >= 0 && pages < p.n_pages;
+    }
+    outside = __ballot(!ok);
+  };
+
+  f32x16 acc[4];
+  float m = kChunkFloor, ls = 0.f;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
+
+  // Wave w brings rows 16 w .. 16 w + 15 of a tile (one page), four rows with
+  // each instruction, whose lanes fill 1 KB of LDS in order.  Lane (row a of
+  // the four, slot s) fetches the chunk of 16 bytes that belongs into slot s
+  // of its row: keys are swizzled by the row, values by its last two bits, so
+  // that the reads below touch every LDS bank once.
+  const int a = l >> 4, s = l & 15;
+  const uint32_t step = (uint32_t)(PAGED ? p.hkv : 1) * 256;   // bytes from row to row
+  const uint32_t kbase = a * step + 16 * (s ^ a), vbase = a * step + 16 * (s ^ (a << 2));
+  typedef __attribute__((address_space(1))) const void gvoid;
+  typedef __attribute__((address_space(3))) void lvoid;
+  // Where the wave's rows of tile t start, and how many of them (from the
+  // first on) are in the cache.
+  auto rows_at = [&](int t, int &have) -> int64_t {
+    const int j = cr.first_of(t) + kTile * w;
+    have = cr.pmax + 1 - j;
+    if (have <= 0) return 0;
+    if (!PAGED) return (((int64_t)b * p.hkv + g) * p.ncap + j) * 256;
+    const int i = 4 * (t - held) + w;
+    if (outside >> i & 1) {
+      have = 0;
+      return 0;
+    }
+    return ((int64_t)__builtin_amdgcn_readlane(pages, i) * kTile * p.hkv + g) * 256;
+  };
+  // Keys that no query of the workgroup sees are masked whatever they are, so
+  // only what lies outside the cache is replaced; values are replaced
+  // wherever none sees them: a weight of 0 times NaN would not be 0.
+  auto bring = [&](const char *src, int have, int off, int flip, u32x4 *to, int hide0, int hide1) {
+    char *dst = (char *)(to + 256 * w);
+    if (have >= kTile && hide0 >= hide1) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        __builtin_amdgcn_global_load_lds((gvoid *)(src + 4 * i * step + (off ^ (flip * i))),
+                                         (lvoid *)(dst + 1024 * i), 16, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const char *at = src + 4 * i * step + (off ^ (flip * i));
+        const int r = 4 * i + a;
+        if (r >= have || (r >= hide0 && r < hide1)) at = (const char *)&chunk_zeros[s];
+        __builtin_amdgcn_global_load_lds((gvoid *)at, (lvoid *)(dst + 1024 * i), 16, 0, 0);
       }
     }
+  };
+  auto bring_keys = [&](int t, u32x4 *to) {
+    int have;
+    const int64_t at = rows_at(t, have);
+    bring(p.k + at, have, kbase, 64, to, 0, 0);
+  };
+  auto bring_values = [&](int t, u32x4 *to) {
+    int have;
+    const int64_t at = rows_at(t, have);
+    const int j = cr.first_of(t) + kTile * w;
+    bring(p.v + at, have, vbase, 0, to, max(0, cr.sink - j), min(kTile, cr.lo - j));
+  };
+
+  auto scores = [&](const u32x4 *tile, f32x16 sc[2]) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[y][r] = 0.f;
+      const int krow = 32 * y + col;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        sc[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            frag(tile[krow * 16 + ((2 * i + half) ^ (krow & 15))]), frag(q[i]), sc[y], 0, 0, 0);
+    }
+  };
+  // Masks the scores of tile t and moves the maximum if it has to.
+  auto settle = [&](f32x16 sc[2], int t) {
+    const int j0 = cr.first_of(t);
+    const uint32_t gone = PAGED ? (uint32_t)(outside >> (4 * (t - held))) & 15u : 0u;
+    const bool whole = !gone && j0 + kChunkKeys <= wmin + 1 &&
+                       (j0 + kChunkKeys <= p.n_sink || j0 > wmax - p.window);
+    if (!whole) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = j0 + 32 * y + 8 * (r >> 2) + 4 * half + (r & 3);
+          const bool sees = (j < row.first) | ((uint32_t)(row.pos - j) < (uint32_t)p.window);
+          const bool there = !(gone >> (2 * y + (r >> 3)) & 1);
+          sc[y][r] = (sees & there) ? sc[y][r] : -__builtin_inff();
+        }
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int r = 1; r < 32; ++r) top = fmaxf(top, sc[r >> 4][r & 15]);
+    if (__ballot(top * p.scale2 > m + kChunkSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top * p.scale2);
+      const float f = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      ls *= f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] *= f;
+    }
+  };
+  // The weights round to bfloat16, as the values are: half a step, 2^-8
+  // relative at most, independent from position to position.
+  auto add = [&](const u32x4 *tile, f32x16 sc[2]) {
+    const int i16 = l & 15, c16 = (l >> 4) & 1;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {   // 16 positions at a time
+      uint32_t pw[4];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float z = __builtin_amdgcn_exp2f(fmaf(sc[x >> 1][8 * (x & 1) + r], p.scale2, -m));
+        sc[x >> 1][8 * (x & 1) + r] = z;
+        ls += z;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        pw[r] = pack2(sc[x >> 1][8 * (x & 1) + 2 * r], sc[x >> 1][8 * (x & 1) + 2 * r + 1]);
+      const int vrow = 16 * x + 4 * half + (i16 >> 2);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int chunk = 4 * c + 2 * c16 + ((i16 & 3) >> 1);
+        const char *base = (const char *)tile + 16 * (chunk ^ ((vrow & 3) << 2)) + 8 * (i16 & 1);
+        const u32x2 lo4 = read_columns(base + vrow * 256), hi4 = read_columns(base + (vrow + 8) * 256);
+        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            frag(u32x4{lo4[0], lo4[1], hi4[0], hi4[1]}), frag(u32x4{pw[0], pw[1], pw[2], pw[3]}),
+            acc[c], 0, 0, 0);
+      }
+    }
+    // One matrix instruction, then what the vector unit can do meanwhile
+    // (509 -> 499 us for 6618 tokens of 32 heads over a window of 4096).
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // matrix
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // LDS reads
+      __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);   // vector, transcendental
+    }
+  };
+
+  if (cr.t0 < cr.t1) {
+    f32x16 sa[2], sb[2];
+    hold_pages(cr.t0);
+    bring_keys(cr.t0, lds.k[0]);
+    bring_values(cr.t0, lds.v[0]);
+    if (cr.t0 + 1 < cr.t1) bring_keys(cr.t0 + 1, lds.k[1]);
     __syncthreads();
+    scores(lds.k[0], sa);
+    settle(sa, cr.t0);
+    __syncthreads();
+    // Tile t's scores are in `now`: bring the tiles after it, score the next
+    // one, and add this one's values.
+    auto round = [&](int t, int par, f32x16 *now, f32x16 *next) {
+      if (t + 1 < cr.t1) bring_values(t + 1, lds.v[par ^ 1]);
+      const bool ends = PAGED && t + 2 >= held + 16;   // the held pages end before tile t + 2
+      if (t + 2 < cr.t1 && !ends) bring_keys(t + 2, lds.k[par]);
+      scores(lds.k[par ^ 1], next);   // (past the last tile: of an old one, unused)
+      add(lds.v[par], now);
+      if (t + 1 < cr.t1) settle(next, t + 1);
+      if (t + 2 < cr.t1 && ends) {
+        hold_pages(t + 2);
+        bring_keys(t + 2, lds.k[par]);
+      }
+      __syncthreads();
+    };
+    for (int t = cr.t0; t < cr.t1; t += 2) {
+      round(t, 0, sa, sb);
+      if (t + 1 < cr.t1) round(t + 1, 1, sb, sa);
+    }
   }
 
   ls += __shfl_xor(ls, 32);
-  if (!live) return;
+  if (!row.live) return;
+  if (p.nsplit > 1) {
+    float *pp = p.part + (row.at / kHeadDim * p.nsplit + split) * kPartStride;
+    if (half == 0) {
+      pp[0] = m;
+      pp[1] = ls;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pp[2 + 32 * c + 8 * (r >> 2) + 4 * half + (r & 3)] = acc[c][r];
+    return;
+  }
   const float inv = ls > 0.f ? 1.f / ls : 0.f;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t at = qat + 32 * c + 8 * i + 4 * half;
-      const float x0 = acc[c][4 * i] * inv, x1 = acc[c][4 * i + 1] * inv;
-      const float x2 = acc[c][4 * i + 2] * inv, x3 = acc[c][4 * i + 3] * inv;
-      if (F32) *(f32x4 *)((float *)p.out + at) = f32x4{x0, x1, x2, x3};
-      else *(u32x2 *)((uint16_t *)p.out + at) = u32x2{pack2(x0, x1), pack2(x2, x3)};
-    }
+    for (int i = 0; i < 4; ++i)
+      *(u32x2 *)((uint16_t *)p.out + row.at + 32 * c + 8 * i + 4 * half) =
+          u32x2{pack2(acc[c][4 * i] * inv, acc[c][4 * i + 1] * inv),
+                pack2(acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv)};
+}
+
+// Joins the splits of one row for each wave.
+template <bool F32>
+__global__ __launch_bounds__(kBlock) void k_chunk_merge(WindowParams p) {
+  ChunkItem it;
+  const int g = (int)(blockIdx.x % (uint32_t)p.hkv);
+  if (!chunk_item<kWaves>(p, (int)(blockIdx.x / (uint32_t)p.hkv), it)) return;
+  const int l = lane_id();
+  const ChunkRow row(p, it, it.row0 + __builtin_amdgcn_readfirstlane(wave_id()), g, 0, 0);
+  if (!row.live) return;
+  const Joined v = join_splits(p.part + row.at / kHeadDim * p.nsplit * kPartStride, p.nsplit);
+  if (F32) *(float2 *)((float *)p.out + row.at + 2 * l) = float2{v.x, v.y};
+  else *(uint32_t *)((uint16_t *)p.out + row.at + 2 * l) = pack2(v.x, v.y);
 }
 
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-template <int KIND, bool PAGED>
-static hipError_t launch_chunk(const WindowParams &p, hipStream_t st) {
-  // Row tiles of all sequences: at most one part-filled tile for each.
-  const int64_t tiles = p.n_rows * p.G / kChunkRows + p.batch;
-  const int64_t grid = tiles * p.hkv;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_chunk_attend<KIND, PAGED><<<(unsigned)grid, kBlock, sizeof(ChunkLds<KIND>), st>>>(p);
-  return hipGetLastError();
+// Row tiles of all sequences: at most one part-filled tile for each that has
+// queries.
+static int64_t chunk_tiles(const WindowParams &p, int rows) {
+  return p.n_rows * p.G / rows + std::min<int64_t>(p.batch, p.n_rows);
+}
+
+// Calls with few rows split what they see over workgroups, so that about two
+// workgroups run on each of the 256 compute units, at least four tiles for
+// each.
+void chunk_split(WindowParams &p, int kind) {
+  const bool f32 = kind == kCacheF32;
+  const int64_t keys = f32 ? kF32Keys * kWaves : kChunkKeys;
+  const int64_t blocks = chunk_tiles(p, f32 ? kF32Rows : kChunkRows) * p.hkv;
+  int64_t seen = std::min<int64_t>(p.ncap, (int64_t)p.n_sink + p.window);
+  const int64_t most = seen / (4 * keys);
+  int64_t split = blocks > 0 ? 512 / blocks : 1;
+  split = std::min<int64_t>(split, most);
+  p.nsplit = (int32_t)std::max<int64_t>(split, 1);
 }
 
 hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
-  if (kind == kCacheF32) return paged ? launch_chunk<kCacheF32, true>(p, st) : launch_chunk<kCacheF32, false>(p, st);
-  return paged ? launch_chunk<kCacheBf16, true>(p, st) : launch_chunk<kCacheBf16, false>(p, st);
+  const bool f32 = kind == kCacheF32;
+  const int64_t grid = chunk_tiles(p, f32 ? kF32Rows : kChunkRows) * p.hkv * p.nsplit;
+  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (f32 && paged) k_chunk_f32<true><<<(unsigned)grid, kBlock, 0, st>>>(p);
+  else if (f32) k_chunk_f32<false><<<(unsigned)grid, kBlock, 0, st>>>(p);
+  else if (paged) k_chunk_bf16<true><<<(unsigned)grid, kBlock, sizeof(ChunkStage), st>>>(p);
+  else k_chunk_bf16<false><<<(unsigned)grid, kBlock, sizeof(ChunkStage), st>>>(p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const unsigned merge = (unsigned)(chunk_tiles(p, kWaves) * p.hkv);
+  if (f32) k_chunk_merge<true><<<merge, kBlock, 0, st>>>(p);
+  else k_chunk_merge<false><<<merge, kBlock, 0, st>>>(p);
+  return hipGetLastError();
 }
 
 }  // namespace sd

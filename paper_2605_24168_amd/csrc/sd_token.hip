@@ -22,11 +22,9 @@
 
 namespace sd {
 
-typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
-
-constexpr int kTokenWaves = 4;
-constexpr int kTokenThreads = 64 * kTokenWaves;
+constexpr int kMergeWaves = 4;
 constexpr int kUnits = 256;          // compute units of the chip
+constexpr int kStepsMin = 6;         // steps of a wave that are worth a split
 constexpr float kFloor = -1e30f;     // running maximum before the first position
 constexpr float kSlack = 8.f;        // a maximum moves once a score passes it by 2^8
 
@@ -65,9 +63,9 @@ struct Tile<kCacheF32> {
 };
 template <>
 struct Tile<kCacheQ4> {
-  u32x4 k;
+  u32x4 k, vs;
   uint32_t ks;
-  uint32_t v[4], vs[4];
+  uint32_t v[4];
 };
 
 template <int KIND>
@@ -94,48 +92,52 @@ __device__ __forceinline__ void load_query(const WindowParams &p, int b, int g, 
 }
 
 // Where a tile's rows are: the first row's index in units of rows, and the
-// distance between rows (page layouts with the heads inside a row).
+// distance between rows (more than one in pages with the heads inside).
 struct TilePlace {
   int64_t row0;
-  int32_t stride;
-  int32_t last;   // largest row of the tile that may be read
+  int32_t last;   // contiguous caches: largest row of the tile that may be read
 };
 
-template <int KIND>
+template <int KIND, bool PAGED>
 __device__ __forceinline__ void load_tile(const WindowParams &p, const TilePlace &at, Tile<KIND> &t) {
   const int l = lane_id(), m = l & 15, a = l >> 4;
-  const int kr = m < at.last ? m : at.last;
-  const int64_t krow = at.row0 + (int64_t)kr * at.stride;
-  int64_t vrow[4];
+  const int stride = PAGED && KIND != kCacheQ4 ? p.hkv : 1;
+  constexpr int kBytes = KIND == kCacheF32 ? 512 : (KIND == kCacheBf16 ? 256 : kQ4RowBytes);
+  const char *k = p.k + at.row0 * kBytes, *v = p.v + at.row0 * kBytes;
+  const int krow = (PAGED ? m : min(m, at.last)) * stride;
+  int vrow[4];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int x = 4 * a + r;
-    vrow[r] = at.row0 + (int64_t)(x < at.last ? x : at.last) * at.stride;
-  }
+  for (int r = 0; r < 4; ++r) vrow[r] = (PAGED ? 4 * a + r : min(4 * a + r, at.last)) * stride;
   if constexpr (KIND == kCacheBf16) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      t.k[i] = __builtin_nontemporal_load((const u32x4 *)(p.k + krow * 256 + 64 * i + 16 * a));
+      t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + (uint32_t)(krow * 256 + 64 * i + 16 * a)));
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      t.v[r] = __builtin_nontemporal_load((const u32x4 *)(p.v + vrow[r] * 256 + 16 * m));
+      t.v[r] = __builtin_nontemporal_load((const u32x4 *)(v + (uint32_t)(vrow[r] * 256 + 16 * m)));
   } else if constexpr (KIND == kCacheF32) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      t.k[i] = __builtin_nontemporal_load((const u32x4 *)(p.k + krow * 512 + 64 * i + 16 * a));
+      t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + (uint32_t)(krow * 512 + 64 * i + 16 * a)));
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        t.v[r][j] = __builtin_nontemporal_load((const u32x4 *)(p.v + vrow[r] * 512 + 256 * j + 16 * m));
+        t.v[r][j] =
+            __builtin_nontemporal_load((const u32x4 *)(v + (uint32_t)(vrow[r] * 512 + 256 * j + 16 * m)));
   } else {
-    t.k = __builtin_nontemporal_load((const u32x4 *)(p.k + krow * kQ4RowBytes + 16 * a));
-    t.ks = (uint32_t)p.ks[krow * kQ4Scales + a];
+    const uint8_t *ks = p.ks + at.row0 * kQ4Scales, *vs = p.vs + at.row0 * kQ4Scales;
+    t.k = __builtin_nontemporal_load((const u32x4 *)(k + (uint32_t)(krow * kQ4RowBytes + 16 * a)));
+    t.ks = (uint32_t)ks[(uint32_t)(krow * kQ4Scales + a)];
+    if (PAGED) {  // the quarter's four rows of scales are one run
+      t.vs = *(const u32x4 *)(vs + (uint32_t)(16 * a));
+    } else {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      t.v[r] = __builtin_nontemporal_load((const uint32_t *)(p.v + vrow[r] * kQ4RowBytes + 4 * m));
-      t.vs[r] = *(const uint32_t *)(p.vs + vrow[r] * kQ4Scales);
+      for (int r = 0; r < 4; ++r) t.vs[r] = *(const uint32_t *)(vs + (uint32_t)(vrow[r] * kQ4Scales));
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      t.v[r] = __builtin_nontemporal_load((const uint32_t *)(v + (uint32_t)(vrow[r] * kQ4RowBytes + 4 * m)));
   }
 }
 
@@ -189,7 +191,8 @@ __device__ __forceinline__ void drop_row(Tile<KIND> &t, int r) {
   } else if constexpr (KIND == kCacheBf16) {
     t.v[r] = u32x4{0u, 0u, 0u, 0u};
   } else {
-    t.v[r] = t.vs[r] = 0u;
+    t.v[r] = 0u;
+    t.vs[r] = 0u;
   }
 }
 
@@ -198,10 +201,6 @@ __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) {
   return __builtin_amdgcn_perm(b, a, 0x07060302u);
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return (uint32_t)f32_to_bf16_rne(a) | ((uint32_t)f32_to_bf16_rne(b) << 16);
 }
 
 // O^T += V^T p^T over two tiles.  acc[e] holds, in lane (head, quarter a),
@@ -223,8 +222,8 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
     // The weights are rounded to bfloat16 (half a step, 2^-9 relative), as
     // the values are: the rounding errors of a row's weights are independent
     // and the output's own rounding is as large.
-    const bf16x8 w = as_bf16(u32x4{pack_bf16(pa[0], pa[1]), pack_bf16(pa[2], pa[3]),
-                                   pack_bf16(pb[0], pb[1]), pack_bf16(pb[2], pb[3])});
+    const bf16x8 w = as_bf16(u32x4{pack2(pa[0], pa[1]), pack2(pa[2], pa[3]),
+                                   pack2(pb[0], pb[1]), pack2(pb[2], pb[3])});
     uint32_t x[8][4];  // channel pairs 2d, 2d + 1 of this lane's 8 rows
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -236,8 +235,9 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
         }
       } else {
         const int sh = 8 * ((lane_id() & 15) >> 2);
-        q4_values(ta.v[r], __uint_as_float((ta.vs[r] >> sh & 255u) << 23), x[r]);
-        q4_values(tb.v[r], __uint_as_float((tb.vs[r] >> sh & 255u) << 23), x[4 + r]);
+        const uint32_t sa = ta.vs[r], sb = tb.vs[r];
+        q4_values(ta.v[r], __uint_as_float((sa >> sh & 255u) << 23), x[r]);
+        q4_values(tb.v[r], __uint_as_float((sb >> sh & 255u) << 23), x[4 + r]);
       }
     }
 #pragma unroll
@@ -255,34 +255,39 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
 }
 
 // LDS of the end of a workgroup: each wave's maxima, sums and outputs.
-__host__ __device__ constexpr size_t token_lds_bytes(int G) {
-  return sizeof(float) * kTokenWaves * (size_t)G * (kHeadDim + 4 + 2);
+__host__ __device__ constexpr size_t token_lds_bytes(int G, int waves) {
+  return sizeof(float) * waves * (size_t)G * (kHeadDim + 4 + 2);
 }
 
-__device__ __forceinline__ void store_out(const WindowParams &p, int kind, int64_t at, float x) {
-  if (kind == kCacheF32) ((float *)p.out)[at] = x;
+template <int KIND>
+__device__ __forceinline__ void store_out(const WindowParams &p, int64_t at, float x) {
+  if (KIND == kCacheF32) ((float *)p.out)[at] = x;
   else ((uint16_t *)p.out)[at] = f32_to_bf16_rne(x);
 }
 
-// grid: splits fastest, then KV heads, then sequences.
-template <int KIND, bool PAGED>
-__global__ __launch_bounds__(kTokenThreads) void k_token_attend(WindowParams p) {
+// grid: splits fastest, then KV heads, then sequences.  The waves of a
+// workgroup take the steps of two tiles in turn, each with the loads of its
+// next step under way while it computes.
+template <int KIND, bool PAGED, int NW>
+__global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_attend(WindowParams p) {
   extern __shared__ float lds[];
-  const int s = (int)(blockIdx.x % p.nsplit);
-  const int g = (int)(blockIdx.x / p.nsplit % p.hkv);
-  const int b = (int)(blockIdx.x / p.nsplit / p.hkv);
-  const int L = clamp_len(p.seq_lens, b, p.ncap);
+  uint32_t i0 = blockIdx.x;
+  const int s = (int)(i0 % (uint32_t)p.nsplit);
+  i0 /= (uint32_t)p.nsplit;
+  const int g = (int)(i0 % (uint32_t)p.hkv), b = (int)(i0 / (uint32_t)p.hkv);
+  const int L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, b, p.ncap));
   const TileRange tr = tile_range(L, p.n_sink, p.window);
   const int nsp = (tr.n + p.span - 1) / p.span;  // splits of this sequence
   if (s > 0 && s >= nsp) return;
   const int64_t orow = (int64_t)b * p.hq + (int64_t)g * p.G;
   if (nsp == 0) {
-    for (int i = threadIdx.x; i < p.G * kHeadDim; i += kTokenThreads)
-      store_out(p, KIND, orow * kHeadDim + i, 0.f);
+    for (int i = threadIdx.x; i < p.G * kHeadDim; i += 64 * NW)
+      store_out<KIND>(p, orow * kHeadDim + i, 0.f);
     return;
   }
   const int t0 = s * p.span, t1 = min(tr.n, t0 + p.span);
-  const int l = lane_id(), a = l >> 4, w = wave_id();
+  const int l = lane_id(), a = l >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(wave_id());
 
   QRegs<KIND> qr;
   load_query<KIND>(p, b, g, qr);
@@ -292,59 +297,67 @@ __global__ __launch_bounds__(kTokenThreads) void k_token_attend(WindowParams p) 
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // The tile's place, and whether its positions can be seen at all.
-  auto place = [&](int t, bool &ok) {
-    TilePlace at;
-    const int pt = tr.tile(t);
-    ok = t < t1;
-    if (PAGED) {
-      int page = ok ? p.block_table[(int64_t)b * p.max_pages + pt] : 0;
-      if (page < 0 || page >= p.n_pages) {
-        page = 0;
-        ok = false;
-      }
-      if (KIND == kCacheQ4) {
-        at.row0 = ((int64_t)page * p.hkv + g) * kTile;
-        at.stride = 1;
-      } else {
-        at.row0 = (int64_t)page * kTile * p.hkv + g;
-        at.stride = p.hkv;
-      }
-      at.last = kTile - 1;
-    } else {
-      const int first = ok ? pt * kTile : 0;
-      at.row0 = ((int64_t)b * p.hkv + g) * p.ncap + first;
-      at.stride = 1;
-      at.last = min(kTile - 1, L - 1 - first);
+  // Step i of this wave: tiles tile_of(i, 0) and the one after it.  Pages: 32
+  // steps at a time, a tile per lane; outside: a bit for each that is not in
+  // the pool.
+  auto tile_of = [&](int i, int u) { return t0 + 2 * (i * NW + w) + u; };
+  const int steps = t0 + 2 * w < t1 ? (t1 - t0 - 2 * w + 2 * NW - 1) / (2 * NW) : 0;
+  int pages = 0;
+  uint64_t outside = 0;
+  auto hold_pages = [&](int i) {
+    if (!PAGED || (i & 31)) return;
+    const int t = tile_of(i + (l >> 1), l & 1);
+    pages = 0;
+    bool ok = true;
+    if (t < t1) {
+      pages = p.block_table[(int64_t)b * p.max_pages + tr.tile(t)];
+      ok = pages >= 0 && pages < p.n_pages;
     }
-    return at;
+    pages = ok ? pages : 0;
+    outside = __ballot(!ok);
   };
-
-  for (int t = t0 + 2 * w; t < t1; t += 2 * kTokenWaves) {
+  struct Step {
     Tile<KIND> tile[2];
-    bool ok[2];
+    bool ok[2];   // the tile is one of this split's and its page in the pool
+  };
+  auto load = [&](int i, Step &st) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const TilePlace at = place(t + u, ok[u]);
-      load_tile<KIND>(p, at, tile[u]);
+      const int t = tile_of(i, u);
+      st.ok[u] = t < t1;
+      TilePlace at;
+      if (PAGED) {
+        const int slot = 2 * (i & 31) + u;
+        st.ok[u] = st.ok[u] && !(outside >> slot & 1);
+        const int64_t page = __builtin_amdgcn_readlane(pages, slot);
+        at.row0 = KIND == kCacheQ4 ? (page * p.hkv + g) * kTile : page * kTile * p.hkv + g;
+        at.last = kTile - 1;
+      } else {
+        const int first = st.ok[u] ? tr.tile(t) * kTile : 0;
+        at.row0 = ((int64_t)b * p.hkv + g) * p.ncap + first;
+        at.last = min(kTile - 1, L - 1 - first);
+      }
+      load_tile<KIND, PAGED>(p, at, st.tile[u]);
     }
+  };
+  auto compute = [&](int i, Step &st) {
     float z[2][4];
     float top = -__builtin_inff();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const f32x4 sc = tile_scores<KIND>(qr, tile[u]);
-      const int j0 = tr.tile(t + u) * kTile;
-      const bool whole = ok[u] && j0 + kTile <= L && (j0 + kTile <= tr.ns || j0 >= tr.lo);
+      const f32x4 sc = tile_scores<KIND>(qr, st.tile[u]);
+      const int j0 = tr.tile(tile_of(i, u)) * kTile;
+      const bool whole = st.ok[u] && j0 + kTile <= L && (j0 + kTile <= tr.ns || j0 >= tr.lo);
 #pragma unroll
       for (int r = 0; r < 4; ++r) z[u][r] = sc[r];
       if (!whole) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int j = j0 + 4 * a + r;
-          const bool sees = ok[u] && j < L && (j < tr.ns || j >= tr.lo);
+          const bool sees = st.ok[u] & (j < L) & ((j < tr.ns) | (j >= tr.lo));
           if (!sees) {
             z[u][r] = -__builtin_inff();
-            drop_row<KIND>(tile[u], r);
+            drop_row<KIND>(st.tile[u], r);
           }
         }
       }
@@ -371,14 +384,30 @@ __global__ __launch_bounds__(kTokenThreads) void k_token_attend(WindowParams p) 
         pw[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], p.scale2, -m));
         ls += pw[u][r];
       }
-    add_values<KIND>(acc, tile[0], tile[1], pw[0], pw[1]);
+    add_values<KIND>(acc, st.tile[0], st.tile[1], pw[0], pw[1]);
+  };
+
+  Step sa, sb;
+  if (steps > 0) {
+    hold_pages(0);
+    load(0, sa);
+  }
+  for (int i = 0; i < steps; i += 2) {   // (an even number of steps between two sets of pages)
+    if (i + 1 < steps) load(i + 1, sb);
+    compute(i, sa);
+    if (i + 1 >= steps) break;
+    if (i + 2 < steps) {
+      hold_pages(i + 2);
+      load(i + 2, sa);
+    }
+    compute(i + 1, sb);
   }
 
   // Join the waves: per head a common maximum, scaled sums and outputs.
   ls += __shfl_xor(ls, 16);
   ls += __shfl_xor(ls, 32);
   const int h = l & 15;
-  float *ml = lds, *o = lds + 2 * kTokenWaves * p.G;
+  float *ml = lds, *o = lds + 2 * NW * p.G;
   constexpr int kRow = kHeadDim + 4;  // heads start 4 banks apart
   if (h < p.G) {
     if (a == 0) {
@@ -395,20 +424,20 @@ __global__ __launch_bounds__(kTokenThreads) void k_token_attend(WindowParams p) 
       }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < p.G * kHeadDim; i += kTokenThreads) {
+  for (int i = threadIdx.x; i < p.G * kHeadDim; i += 64 * NW) {
     const int hh = i / kHeadDim, c = i % kHeadDim;
     float M = kFloor;
 #pragma unroll
-    for (int x = 0; x < kTokenWaves; ++x) M = fmaxf(M, ml[2 * (x * p.G + hh)]);
+    for (int x = 0; x < NW; ++x) M = fmaxf(M, ml[2 * (x * p.G + hh)]);
     float sum = 0.f, v = 0.f;
 #pragma unroll
-    for (int x = 0; x < kTokenWaves; ++x) {
+    for (int x = 0; x < NW; ++x) {
       const float f = __builtin_amdgcn_exp2f(ml[2 * (x * p.G + hh)] - M);
       sum += f * ml[2 * (x * p.G + hh) + 1];
       v += f * o[(x * p.G + hh) * kRow + c];
     }
     if (nsp == 1) {
-      store_out(p, KIND, (orow + hh) * kHeadDim + c, sum > 0.f ? v / sum : 0.f);
+      store_out<KIND>(p, (orow + hh) * kHeadDim + c, sum > 0.f ? v / sum : 0.f);
     } else {
       float *pp = p.part + ((orow + hh) * p.nsplit + s) * kPartStride;
       if (c == 0) {
@@ -420,42 +449,43 @@ __global__ __launch_bounds__(kTokenThreads) void k_token_attend(WindowParams p) 
   }
 }
 
-// Joins the splits of each query head: partials (maximum in powers of two,
-// sum, 128 unnormalised channels).  One workgroup per query head; sequences of
-// one split are done already.
-__global__ __launch_bounds__(kHeadDim) void k_token_merge(WindowParams p, int kind) {
-  const int64_t row = blockIdx.x;
-  const int b = (int)(row / p.hq);
-  const TileRange tr = tile_range(clamp_len(p.seq_lens, b, p.ncap), p.n_sink, p.window);
+// Joins the splits of each query head, one wave each; sequences of one split
+// are done already.
+template <int KIND>
+__global__ __launch_bounds__(64 * kMergeWaves) void k_token_merge(WindowParams p) {
+  const int row = (int)blockIdx.x * kMergeWaves + __builtin_amdgcn_readfirstlane(wave_id());
+  if (row >= p.batch * p.hq) return;
+  const TileRange tr =
+      tile_range(clamp_len(p.seq_lens, row / p.hq, p.ncap), p.n_sink, p.window);
   const int nsp = (tr.n + p.span - 1) / p.span;
   if (nsp <= 1) return;
-  const float *pp = p.part + row * p.nsplit * kPartStride;
-  const int c = threadIdx.x;
-  float M = kFloor;
-  for (int i = 0; i < nsp; ++i) M = fmaxf(M, pp[(int64_t)i * kPartStride]);
-  float sum = 0.f, v = 0.f;
-  for (int i = 0; i < nsp; ++i) {
-    const float *x = pp + (int64_t)i * kPartStride;
-    const float f = __builtin_amdgcn_exp2f(x[0] - M);
-    sum += f * x[1];
-    v += f * x[2 + c];
-  }
-  store_out(p, kind, row * kHeadDim + c, sum > 0.f ? v / sum : 0.f);
+  const Joined v = join_splits(p.part + (int64_t)row * p.nsplit * kPartStride, nsp);
+  const int64_t at = (int64_t)row * kHeadDim + 2 * lane_id();
+  store_out<KIND>(p, at, v.x);
+  store_out<KIND>(p, at + 1, v.y);
 }
 
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
+// Waves of a workgroup: eight; four where the heads' outputs of eight would not
+// leave LDS for a second workgroup (more than eight heads to a KV head), and
+// for float32, whose two steps in registers leave room for one wave per SIMD.
+static int token_waves(const WindowParams &p, int kind) {
+  return p.G <= 8 && kind != kCacheF32 ? 8 : 4;
+}
+
 void window_split(WindowParams &p, int kind) {
-  (void)kind;
+  const int waves = token_waves(p, kind);
   const int64_t cap = (p.ncap + kTile - 1) / kTile;
   int64_t tiles = ((int64_t)p.n_sink + kTile - 1) / kTile + ((int64_t)p.window + kTile - 1) / kTile + 1;
   if (tiles > cap) tiles = cap;
   if (tiles < 1) tiles = 1;
   const int64_t items = (int64_t)p.batch * p.hkv;
-  const int64_t step = 2 * kTokenWaves;
-  int64_t split = items > 0 ? (4LL * kUnits + items - 1) / items : 1;
-  const int64_t most = (tiles + step - 1) / step;
+  const int64_t step = 2 * waves;
+  const int64_t target = 4 * kUnits * 4 / waves;
+  int64_t split = items > 0 ? (target + items - 1) / items : 1;
+  const int64_t most = (tiles + step * kStepsMin - 1) / (step * kStepsMin);
   split = split < 1 ? 1 : (split > most ? most : split);
   int64_t span = (tiles + split - 1) / split;
   span = (span + step - 1) / step * step;
@@ -463,22 +493,31 @@ void window_split(WindowParams &p, int kind) {
   p.nsplit = (int32_t)((tiles + span - 1) / span);
 }
 
-template <int KIND, bool PAGED>
+template <int KIND, bool PAGED, int NW>
 static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
   const int64_t grid = (int64_t)p.batch * p.hkv * p.nsplit;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_token_attend<KIND, PAGED><<<(unsigned)grid, kTokenThreads, token_lds_bytes(p.G), st>>>(p);
+  k_token_attend<KIND, PAGED, NW><<<(unsigned)grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
-  k_token_merge<<<(unsigned)(p.batch * p.hq), kHeadDim, 0, st>>>(p, KIND);
+  const unsigned rows = (unsigned)(p.batch * p.hq);
+  k_token_merge<KIND><<<(rows + kMergeWaves - 1) / kMergeWaves, 64 * kMergeWaves, 0, st>>>(p);
   return hipGetLastError();
+}
+
+template <int KIND>
+static hipError_t launch_token_kind(const WindowParams &p, bool paged, hipStream_t st) {
+  if constexpr (KIND != kCacheF32)
+    if (token_waves(p, KIND) == 8)
+      return paged ? launch_token<KIND, true, 8>(p, st) : launch_token<KIND, false, 8>(p, st);
+  return paged ? launch_token<KIND, true, 4>(p, st) : launch_token<KIND, false, 4>(p, st);
 }
 
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
   switch (kind) {
-    case kCacheF32: return paged ? launch_token<kCacheF32, true>(p, st) : launch_token<kCacheF32, false>(p, st);
-    case kCacheBf16: return paged ? launch_token<kCacheBf16, true>(p, st) : launch_token<kCacheBf16, false>(p, st);
-    default: return paged ? launch_token<kCacheQ4, true>(p, st) : launch_token<kCacheQ4, false>(p, st);
+    case kCacheF32: return launch_token_kind<kCacheF32>(p, paged, st);
+    case kCacheBf16: return launch_token_kind<kCacheBf16>(p, paged, st);
+    default: return launch_token_kind<kCacheQ4>(p, paged, st);
   }
 }
 
