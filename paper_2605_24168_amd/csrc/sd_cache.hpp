@@ -97,18 +97,29 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 struct Joined {
   float x, y;
 };
+// Partials that one workgroup writes and another of the same launch reads:
+// past the caches that are not common to both.
+__device__ __forceinline__ void put_shared(float *at, float x) {
+  __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool SHARED>
+__device__ __forceinline__ float get_partial(const float *at) {
+  if (SHARED) return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return *at;
+}
+template <bool SHARED>
 __device__ __forceinline__ Joined join_splits(const float *pp, int n) {
   const int l = lane_id();
   float m = -3e38f;
-  for (int s = l; s < n; s += 64) m = fmaxf(m, pp[(int64_t)s * kPartStride]);
+  for (int s = l; s < n; s += 64) m = fmaxf(m, get_partial<SHARED>(pp + (int64_t)s * kPartStride));
   const float M = wave_max(m);
   float sum = 0.f, x = 0.f, y = 0.f;
   for (int s0 = 0; s0 < n; s0 += 64) {
     const int s = s0 + l;
     float f = 0.f;
     if (s < n) {
-      f = __builtin_amdgcn_exp2f(pp[(int64_t)s * kPartStride] - M);
-      sum += f * pp[(int64_t)s * kPartStride + 1];
+      f = __builtin_amdgcn_exp2f(get_partial<SHARED>(pp + (int64_t)s * kPartStride) - M);
+      sum += f * get_partial<SHARED>(pp + (int64_t)s * kPartStride + 1);
     }
     const int k = n - s0 < 64 ? n - s0 : 64;
     const float *o = pp + (int64_t)s0 * kPartStride + 2 + 2 * l;
@@ -117,7 +128,8 @@ __device__ __forceinline__ Joined join_splits(const float *pp, int n) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int64_t j = i0 + i < k ? i0 + i : k - 1;
-        v[i] = float2{o[j * kPartStride], o[j * kPartStride + 1]};
+        v[i] = float2{get_partial<SHARED>(o + j * kPartStride),
+                      get_partial<SHARED>(o + j * kPartStride + 1)};
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -567,7 +567,7 @@ __global__ __launch_bounds__(kBlock) void k_chunk_merge(WindowParams p) {
   const int l = lane_id();
   const ChunkRow row(p, it, it.row0 + __builtin_amdgcn_readfirstlane(wave_id()), g, 0, 0);
   if (!row.live) return;
-  const Joined v = join_splits(p.part + row.at / kHeadDim * p.nsplit * kPartStride, p.nsplit);
+  const Joined v = join_splits<false>(p.part + row.at / kHeadDim * p.nsplit * kPartStride, p.nsplit);
   if (F32) *(float2 *)((float *)p.out + row.at + 2 * l) = float2{v.x, v.y};
   else *(uint32_t *)((uint16_t *)p.out + row.at + 2 * l) = pack2(v.x, v.y);
 }

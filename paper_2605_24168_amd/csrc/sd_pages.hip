@@ -5,8 +5,8 @@
 // latency of a few dependent reads; only the copies move bytes that matter.
 // Free pages are taken lowest first, which makes results independent of the
 // order of workgroups: a first kernel counts the free pages of every stretch
-// of the pool, one workgroup turns counts and requests into ranks, and a third
-// hands the free pages out by rank.
+// of the pool, and the workgroup that finishes last turns counts and requests
+// into ranks; the next one hands the free pages out by rank.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,9 +16,9 @@
 
 namespace sd {
 
-constexpr int kStretch = 4096;                    // pages counted by one workgroup
-constexpr int kPerThread = kStretch / kBlock;     // consecutive pages of a thread
-constexpr int kPlan = 1024;                       // threads of the planning workgroup
+constexpr int kPlan = 1024;                       // threads that count and plan
+constexpr int kPerThread = 4;                     // consecutive pages of a thread
+constexpr int kStretch = kPlan * kPerThread;      // pages counted by one workgroup
 constexpr int64_t kPiece = 16 * 1024;             // bytes a workgroup copies at once
 constexpr int kMany = 1 << 29;                    // more than any number of pages
 
@@ -29,8 +29,9 @@ struct PageWork {
   int32_t *first;     // [batch]: extend: rank of the row's first page
   int32_t *have;      // [batch]: extend: pages it held; fork: children of a parent
   int32_t *eldest;    // [batch]: fork: a parent's first child
-  int32_t *list;      // [pages]: fork: child of each rank; compact: movers
-  int32_t *hole;      // [pages]: compact: holes; fork: [0, batch) fresh pages, [batch, ..) old ones
+  int32_t *list;      // [pages]: compact: movers; fork: a child's own last page
+  int32_t *hole;      // [pages]: compact: holes; fork: [0, batch) a child's rank among those
+                      // that get a page, [batch, ..) the page that it copies
 };
 enum { kLimit = 0, kMoves = 1, kLive = 2 };
 
@@ -46,7 +47,7 @@ static size_t carve_pages(int64_t n_pages, int64_t batch, char *base, PageWork *
     return (int32_t *)ptr;
   };
   PageWork x;
-  x.base = take(stretches(n_pages));
+  x.base = take(stretches(n_pages) + 1);
   x.scalar = take(8);
   x.first = take(batch);
   x.have = take(batch);
@@ -72,29 +73,43 @@ __device__ __forceinline__ bool in_pool(const PagesParams &p, int page) {
 template <bool LIVE>
 __device__ __forceinline__ uint32_t stretch_bits(const PagesParams &p, int s) {
   const int64_t i0 = (int64_t)s * kStretch + threadIdx.x * kPerThread;
+  int x[kPerThread];
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) x[i] = i0 + i < p.n_pages ? p.refs[i0 + i] : (LIVE ? 0 : 1);
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    const int64_t page = i0 + i;
-    if (page < p.n_pages && (LIVE ? p.refs[page] > 0 : p.refs[page] == 0)) m |= 1u << i;
-  }
+  for (int i = 0; i < kPerThread; ++i) m |= (LIVE ? x[i] > 0 : x[i] == 0) ? 1u << i : 0u;
   return m;
 }
 
+// Workgroups of the counting launch that are done; 0 between calls.
+static __device__ uint32_t stretches_done;
+
+// Counts this workgroup's stretch; true for the workgroup that counts last,
+// which finds all counts in w.base.  (They are stored past the caches that
+// workgroups do not share, and have arrived before a workgroup counts itself.)
 template <bool LIVE>
-__global__ __launch_bounds__(kBlock) void k_pages_count(PagesParams p, PageWork w) {
-  __shared__ int tmp[kWaves];
+__device__ __forceinline__ bool count_stretch(const PagesParams &p, const PageWork &w, int *tmp) {
+  __shared__ uint32_t before;
   int total;
-  block_excl_scan(__popc(stretch_bits<LIVE>(p, blockIdx.x)), tmp, &total);
-  if (threadIdx.x == 0) w.base[blockIdx.x] = total;
+  block_excl_scan<kPlan>(__popc(stretch_bits<LIVE>(p, blockIdx.x)), tmp, &total);
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(&w.base[blockIdx.x], total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    before = atomicInc(&stretches_done, gridDim.x - 1);
+  }
+  __syncthreads();
+  return before == gridDim.x - 1;
 }
 
-// Counts of the stretches to the pages before each; returns all of them.
-__device__ __forceinline__ int plan_bases(const PageWork &w, int n, int *tmp) {
+// Counts of the launch's stretches to the pages before each; returns all of
+// them.
+__device__ __forceinline__ int plan_bases(const PageWork &w, int *tmp) {
+  const int n = (int)gridDim.x;
   int before = 0;
   for (int i0 = 0; i0 < n; i0 += kPlan) {
     const int i = i0 + threadIdx.x;
-    const int c = i < n ? w.base[i] : 0;
+    const int c = i < n ? __hip_atomic_load(&w.base[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
     int total;
     const int x = block_excl_scan<kPlan>(c, tmp, &total);
     if (i < n) w.base[i] = before + x;
@@ -110,7 +125,8 @@ __global__ __launch_bounds__(kPlan) void k_extend_plan(PagesParams p, PageWork w
                                                        const int32_t *grow, int32_t *status) {
   __shared__ int tmp[kPlan / 64];
   __shared__ int limit;
-  const int nfree = plan_bases(w, (int)((p.n_pages + kStretch - 1) / kStretch), tmp);
+  if (!count_stretch<false>(p, w, tmp)) return;
+  const int nfree = plan_bases(w, tmp);
   if (threadIdx.x == 0) limit = 0;
   __syncthreads();
   int before = 0;
@@ -146,14 +162,14 @@ __global__ __launch_bounds__(kPlan) void k_extend_plan(PagesParams p, PageWork w
 
 // Rows that get pages are those whose ranks end at or below the limit; their
 // ranks ascend, so a free page finds its row by bisection.
-__global__ __launch_bounds__(kBlock) void k_extend_take(PagesParams p, PageWork w) {
-  __shared__ int tmp[kWaves];
+__global__ __launch_bounds__(kPlan) void k_extend_take(PagesParams p, PageWork w) {
+  __shared__ int tmp[kPlan / 64];
   const int limit = w.scalar[kLimit];
   const int base = w.base[blockIdx.x];
   if (base >= limit) return;
   const uint32_t mine = stretch_bits<false>(p, blockIdx.x);
   int total;
-  int rank = base + block_excl_scan(__popc(mine), tmp, &total);
+  int rank = base + block_excl_scan<kPlan>(__popc(mine), tmp, &total);
   for (uint32_t m = mine; m && rank < limit; m &= m - 1, ++rank) {
     const int page = (int)blockIdx.x * kStretch + threadIdx.x * kPerThread + __ffs(m) - 1;
     int lo = 0, hi = p.batch;  // first row whose ranks start past this one
@@ -175,7 +191,8 @@ __global__ __launch_bounds__(kPlan) void k_fork_plan(PagesParams from, PagesPara
                                                      const int32_t *parents, int keep,
                                                      int32_t *status) {
   __shared__ int tmp[kPlan / 64];
-  const int nfree = plan_bases(w, (int)((from.n_pages + kStretch - 1) / kStretch), tmp);
+  if (!count_stretch<false>(from, w, tmp)) return;
+  const int nfree = plan_bases(w, tmp);
   for (int r = threadIdx.x; r < from.batch; r += kPlan) {
     w.have[r] = 0;
     w.eldest[r] = INT32_MAX;
@@ -186,7 +203,7 @@ __global__ __launch_bounds__(kPlan) void k_fork_plan(PagesParams from, PagesPara
     if (r >= 0 && r < from.batch) atomicMin(&w.eldest[r], i);
   }
   __syncthreads();
-  int32_t *fresh = w.hole, *old = w.hole + to.batch;
+  int32_t *rank_of = w.hole, *old = w.hole + to.batch;
   int before = 0;
   for (int i0 = 0; i0 < to.batch; i0 += kPlan) {
     const int i = i0 + threadIdx.x;
@@ -207,63 +224,63 @@ __global__ __launch_bounds__(kPlan) void k_fork_plan(PagesParams from, PagesPara
       const bool ok = !need || rank < nfree;
       status[i] = ok ? 0 : 1;
       to.seq_lens[i] = ok ? L : 0;
-      fresh[i] = -1;
+      rank_of[i] = need && ok ? rank : -1;
       old[i] = need ? from.table[(int64_t)r * from.max_pages + L / kTile] : -1;
-      if (need && ok) w.list[rank] = i;
       if (ok && r >= 0) atomicAdd(&w.have[r], 1);
       // (what k_fork_rows makes of the row: its parent, or none)
       w.first[i] = ok ? r : -1;
     }
     before += total;
   }
-  if (threadIdx.x == 0) w.scalar[kLimit] = min(before, nfree);
 }
 
-__global__ __launch_bounds__(kBlock) void k_fork_take(PagesParams p, PageWork w) {
-  __shared__ int tmp[kWaves];
-  const int limit = w.scalar[kLimit];
-  const int base = w.base[blockIdx.x];
-  if (base >= limit) return;
-  const uint32_t mine = stretch_bits<false>(p, blockIdx.x);
+// The free page of the given rank: its stretch by bisection over the counts,
+// its place there by a prefix sum (nothing writes refs meanwhile).  Called by
+// a whole workgroup of kBlock threads; sh: LDS.
+__device__ __forceinline__ int page_of_rank(const PagesParams &p, const PageWork &w, int rank, int *tmp,
+                                            int *sh) {
+  const int n = (int)(((int64_t)p.n_pages + kStretch - 1) / kStretch);
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (w.base[mid] <= rank) lo = mid + 1;
+    else hi = mid;
+  }
+  const int s = lo - 1;
+  int left = rank - w.base[s];
+  constexpr int kMine = kStretch / kBlock;
+  const int64_t i0 = (int64_t)s * kStretch + threadIdx.x * kMine;
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i)
+    if (i0 + i < p.n_pages && p.refs[i0 + i] == 0) m |= 1u << i;
   int total;
-  int rank = base + block_excl_scan(__popc(mine), tmp, &total);
-  for (uint32_t m = mine; m && rank < limit; m &= m - 1, ++rank) {
-    const int page = (int)blockIdx.x * kStretch + threadIdx.x * kPerThread + __ffs(m) - 1;
-    w.hole[w.list[rank]] = page;
-    p.refs[page] = 1;
+  left -= block_excl_scan(__popc(m), tmp, &total);
+  if (left >= 0 && left < __popc(m)) {
+    for (; left > 0; --left) m &= m - 1;
+    *sh = (int)i0 + __ffs(m) - 1;
   }
+  __syncthreads();
+  return *sh;
 }
 
-// Workgroups [0, to.batch) write the children's rows, the others count the
-// parents' pages.
-__global__ __launch_bounds__(kBlock) void k_fork_rows(PagesParams from, PagesParams to, PageWork w,
-                                                      int keep) {
+// Row i of `to`: its parent's pages, the last one replaced by a page of its
+// own where it has to be.
+__global__ __launch_bounds__(kBlock) void k_fork_rows(PagesParams from, PagesParams to, PageWork w) {
+  __shared__ int tmp[kWaves], page_sh;
   const int i = blockIdx.x;
-  if (i < to.batch) {
-    const int r = w.first[i];
-    const int L = r >= 0 ? row_len(from, r) : 0;
-    const int full = L / kTile, n = (L + kTile - 1) / kTile;
-    const int fresh = w.hole[i];
-    int32_t *dst = to.table + (int64_t)i * to.max_pages;
-    const int32_t *src = from.table + (int64_t)(r < 0 ? 0 : r) * from.max_pages;
-    for (int c = threadIdx.x; c < to.max_pages; c += kBlock) {
-      int page = -1;
-      if (c < n) page = c == full && fresh >= 0 ? fresh : src[c];
-      dst[c] = page;
-    }
-    return;
+  const int r = w.first[i], rank = w.hole[i];
+  const int L = r >= 0 ? row_len(from, r) : 0;
+  const int full = L / kTile, n = (L + kTile - 1) / kTile;
+  const int fresh = rank >= 0 ? page_of_rank(from, w, rank, tmp, &page_sh) : -1;
+  int32_t *dst = to.table + (int64_t)i * to.max_pages;
+  const int32_t *src = from.table + (int64_t)(r < 0 ? 0 : r) * from.max_pages;
+  for (int c = threadIdx.x; c < to.max_pages; c += kBlock) {
+    int page = -1;
+    if (c < n) page = c == full && fresh >= 0 ? fresh : src[c];
+    dst[c] = page;
   }
-  const int r = i - to.batch;
-  const int L = row_len(from, r), children = w.have[r];
-  const int32_t *src = from.table + (int64_t)r * from.max_pages;
-  const int delta = keep ? children : children - 1;
-  if (delta != 0)
-    for (int c = threadIdx.x; c < L / kTile; c += kBlock)
-      if (in_pool(from, src[c])) atomicAdd(&from.refs[src[c]], delta);
-  if (!keep && children == 0 && L % kTile && threadIdx.x == 0) {
-    const int page = src[L / kTile];
-    if (in_pool(from, page)) atomicAdd(&from.refs[page], -1);
-  }
+  if (threadIdx.x == 0) w.list[i] = fresh;
 }
 
 // Pieces of a page over all pools.
@@ -310,21 +327,37 @@ __device__ __forceinline__ void copy_piece(const Pools &pools, int64_t src, int6
   }
 }
 
-// Workgroups [0, to.batch * pieces) copy the part-filled pages, the others
-// empty the rows that the call ends.
-__global__ __launch_bounds__(kBlock) void k_fork_tails(PagesParams from, PagesParams to, PageWork w,
-                                                       Pools pools, int pieces) {
-  const int64_t i = blockIdx.x;
-  if (i < (int64_t)to.batch * pieces) {
-    const int child = (int)(i / pieces);
-    const int fresh = w.hole[child], old = w.hole[to.batch + child];
-    if (fresh >= 0 && in_pool(from, old)) copy_piece(pools, old, fresh, (int)(i % pieces));
+// Workgroups [0, from.batch) count the pages of the parents' rows, and empty
+// those that the call ends; the others copy the part-filled pages.
+__global__ __launch_bounds__(kBlock) void k_fork_pages(PagesParams from, PagesParams to, PageWork w,
+                                                       Pools pools, int pieces, int keep) {
+  int64_t i = blockIdx.x;
+  if (i < from.batch) {
+    const int r = (int)i;
+    const int L = row_len(from, r), children = w.have[r];
+    int32_t *row = from.table + (int64_t)r * from.max_pages;
+    const int delta = keep ? children : children - 1;
+    // (the page that the first child takes over keeps its count)
+    const int counted = L / kTile + (!keep && children == 0 && L % kTile ? 1 : 0);
+    if (delta != 0)
+      for (int c = threadIdx.x; c < counted; c += kBlock)
+        if (in_pool(from, row[c])) atomicAdd(&from.refs[row[c]], delta);
+    if (!keep) {
+      for (int c = threadIdx.x; c < from.max_pages; c += kBlock) row[c] = -1;
+      __syncthreads();  // (every thread has read the length)
+      if (threadIdx.x == 0) from.seq_lens[r] = 0;
+    }
     return;
   }
-  const int r = (int)(i - (int64_t)to.batch * pieces);
-  int32_t *row = from.table + (int64_t)r * from.max_pages;
-  for (int c = threadIdx.x; c < from.max_pages; c += kBlock) row[c] = -1;
-  if (threadIdx.x == 0) from.seq_lens[r] = 0;
+  i -= from.batch;
+  const int child = (int)(i / (pieces + 1)), piece = (int)(i % (pieces + 1));
+  const int fresh = w.list[child], old = w.hole[to.batch + child];
+  if (fresh < 0) return;
+  if (piece == pieces) {
+    if (threadIdx.x == 0) from.refs[fresh] = 1;
+  } else if (in_pool(from, old)) {
+    copy_piece(pools, old, fresh, piece);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -357,7 +390,8 @@ __global__ __launch_bounds__(kBlock) void k_pages_copy(Pools pools, int64_t n_pa
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(kPlan) void k_compact_plan(PagesParams p, PageWork w, int32_t *n_live) {
   __shared__ int tmp[kPlan / 64];
-  const int n = plan_bases(w, (int)((p.n_pages + kStretch - 1) / kStretch), tmp);
+  if (!count_stretch<true>(p, w, tmp)) return;
+  const int n = plan_bases(w, tmp);
   // Live pages below n: those of the stretches before n's, and of its own.
   __syncthreads();
   const int s = n / kStretch;
@@ -376,12 +410,12 @@ __global__ __launch_bounds__(kPlan) void k_compact_plan(PagesParams p, PageWork 
 
 // Movers and holes in ascending order; a mover's entry of remap holds its rank
 // i as -2 - i until k_compact_move has put the page there.
-__global__ __launch_bounds__(kBlock) void k_compact_lists(PagesParams p, PageWork w, int32_t *remap) {
-  __shared__ int tmp[kWaves];
+__global__ __launch_bounds__(kPlan) void k_compact_lists(PagesParams p, PageWork w, int32_t *remap) {
+  __shared__ int tmp[kPlan / 64];
   const int n = w.scalar[kLive], below = n - w.scalar[kMoves];
   const uint32_t mine = stretch_bits<true>(p, blockIdx.x);
   int total;
-  int live = w.base[blockIdx.x] + block_excl_scan(__popc(mine), tmp, &total);
+  int live = w.base[blockIdx.x] + block_excl_scan<kPlan>(__popc(mine), tmp, &total);
   const int64_t p0 = (int64_t)blockIdx.x * kStretch + threadIdx.x * kPerThread;
   for (int i = 0; i < kPerThread; ++i) {
     const int64_t page = p0 + i;
@@ -437,14 +471,15 @@ __global__ __launch_bounds__(kBlock) void k_compact_move(PagesParams p, PageWork
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
+// Workgroups of a counting launch (one at least: it also plans).
+static unsigned counters(int64_t n_pages) { return (unsigned)std::max<int64_t>(stretches(n_pages), 1); }
+
 hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_t *status,
                                char *work, hipStream_t st) {
   PageWork w;
   carve_pages(p.n_pages, p.batch, work, &w);
-  const unsigned n = (unsigned)stretches(p.n_pages);
-  if (n) k_pages_count<false><<<n, kBlock, 0, st>>>(p, w);
-  k_extend_plan<<<1, kPlan, 0, st>>>(p, w, grow, status);
-  if (n) k_extend_take<<<n, kBlock, 0, st>>>(p, w);
+  k_extend_plan<<<counters(p.n_pages), kPlan, 0, st>>>(p, w, grow, status);
+  k_extend_take<<<counters(p.n_pages), kPlan, 0, st>>>(p, w);
   return hipGetLastError();
 }
 
@@ -453,15 +488,12 @@ hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
                              int32_t *status, char *work, hipStream_t st) {
   PageWork w;
   carve_pages(from.n_pages, from.batch > to.batch ? from.batch : to.batch, work, &w);
-  const unsigned n = (unsigned)stretches(from.n_pages);
   const int pieces = pieces_of(pools);
-  const int64_t tails = (int64_t)to.batch * pieces + (keep ? 0 : from.batch);
-  if (tails > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (n) k_pages_count<false><<<n, kBlock, 0, st>>>(from, w);
-  k_fork_plan<<<1, kPlan, 0, st>>>(from, to, w, parents, keep ? 1 : 0, status);
-  if (n) k_fork_take<<<n, kBlock, 0, st>>>(from, w);
-  k_fork_rows<<<(unsigned)(to.batch + from.batch), kBlock, 0, st>>>(from, to, w, keep ? 1 : 0);
-  if (tails) k_fork_tails<<<(unsigned)tails, kBlock, 0, st>>>(from, to, w, pools, pieces);
+  const int64_t last = from.batch + (int64_t)to.batch * (pieces + 1);
+  if (last > INT32_MAX) return hipErrorInvalidConfiguration;
+  k_fork_plan<<<counters(from.n_pages), kPlan, 0, st>>>(from, to, w, parents, keep ? 1 : 0, status);
+  if (to.batch) k_fork_rows<<<(unsigned)to.batch, kBlock, 0, st>>>(from, to, w);
+  k_fork_pages<<<(unsigned)last, kBlock, 0, st>>>(from, to, w, pools, pieces, keep ? 1 : 0);
   return hipGetLastError();
 }
 
@@ -483,15 +515,14 @@ hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_
                                 int32_t *n_live, char *work, hipStream_t st) {
   PageWork w;
   carve_pages(p.n_pages, p.batch, work, &w);
-  const int64_t n = stretches(p.n_pages);
+  const unsigned n = counters(p.n_pages);
   const int pieces = pieces_of(pools);
-  if (n) k_pages_count<true><<<(unsigned)n, kBlock, 0, st>>>(p, w);
-  k_compact_plan<<<1, kPlan, 0, st>>>(p, w, n_live);
-  if (n) k_compact_lists<<<(unsigned)n, kBlock, 0, st>>>(p, w, remap);
-  const int counters = (int)(n < 64 ? n : 64);
+  k_compact_plan<<<n, kPlan, 0, st>>>(p, w, n_live);
+  k_compact_lists<<<n, kPlan, 0, st>>>(p, w, remap);
+  const int writers = (int)(n < 64 ? n : 64);
   const int64_t movers = std::min<int64_t>((int64_t)p.n_pages / 2 * pieces, 2048);
-  k_compact_move<<<(unsigned)(p.batch + counters + movers), kBlock, 0, st>>>(p, w, pools, remap,
-                                                                            pieces, counters);
+  k_compact_move<<<(unsigned)(p.batch + writers + movers), kBlock, 0, st>>>(p, w, pools, remap,
+                                                                            pieces, writers);
   return hipGetLastError();
 }
 

@@ -9,12 +9,12 @@
 // A wave takes tiles of 16 positions, two at a time, straight from global
 // memory into the operand registers of the matrix unit; no LDS is touched
 // until the end.  With K the first operand, S = K q^T leaves lane (head =
-// lane & 15, quarter = lane >> 4) the scores of positions 4 quarter + r of its
-// tile, r = 0..3.  The weights p = 2^(scale (s - m)) then are, without any
+// lane & 15, quarter = lane >> 4) the scores of positions 4 r + quarter of its
+// tile, r = 0..3 (see row_of).  The weights p = 2^(scale (s - m)) then are, without any
 // move between lanes, the second operand of O^T = V^T p^T over the two tiles,
 // because the order in which a contraction runs is free: slot i of quarter a
-// stands for position 4a + i of the first tile (i < 4) or 4a + i - 4 of the
-// second, and V's rows are loaded in that order.
+// stands for position 4 i + a of the first tile (i < 4) or 4 (i - 4) + a of
+// the second, and V's rows are loaded in that order.
 #include <hip/hip_runtime.h>
 
 #include "sd_cache.hpp"
@@ -22,9 +22,7 @@
 
 namespace sd {
 
-constexpr int kMergeWaves = 4;
 constexpr int kUnits = 256;          // compute units of the chip
-constexpr int kStepsMin = 6;         // steps of a wave that are worth a split
 constexpr float kFloor = -1e30f;     // running maximum before the first position
 constexpr float kSlack = 8.f;        // a maximum moves once a score passes it by 2^8
 
@@ -63,9 +61,9 @@ struct Tile<kCacheF32> {
 };
 template <>
 struct Tile<kCacheQ4> {
-  u32x4 k, vs;
+  u32x4 k;
   uint32_t ks;
-  uint32_t v[4];
+  uint32_t v[4], vs[4];
 };
 
 template <int KIND>
@@ -91,53 +89,58 @@ __device__ __forceinline__ void load_query(const WindowParams &p, int b, int g, 
   }
 }
 
-// Where a tile's rows are: the first row's index in units of rows, and the
-// distance between rows (more than one in pages with the heads inside).
-struct TilePlace {
-  int64_t row0;
-  int32_t last;   // contiguous caches: largest row of the tile that may be read
+// Lane (m = lane & 15, quarter a) reads key row row_of(m) as row m of the
+// first operand, so that its scores are those of rows 4 r + a; the values of
+// one instruction are then four rows in a run.
+__device__ __forceinline__ int row_of(int m) { return 4 * (m & 3) + (m >> 2); }
+
+// Byte offsets of a lane's reads from the tile's first row (rows beyond `last`
+// replaced by it), `stride` rows apart.
+template <int KIND>
+struct Offsets {
+  static constexpr int kBytes = KIND == kCacheF32 ? 512 : (KIND == kCacheBf16 ? 256 : kQ4RowBytes);
+  uint32_t k, v[4], ks, vs[4];
+  __device__ __forceinline__ Offsets(int stride, int last) {
+    const int l = lane_id(), m = l & 15, a = l >> 4;
+    const uint32_t kr = (uint32_t)(min(row_of(m), last) * stride);
+    k = kr * kBytes + 16 * a;
+    ks = kr * kQ4Scales + a;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t vr = (uint32_t)(min(4 * r + a, last) * stride);
+      v[r] = vr * kBytes + (KIND == kCacheQ4 ? 4 : 16) * m;
+      vs[r] = vr * kQ4Scales;
+    }
+  }
 };
 
-template <int KIND, bool PAGED>
-__device__ __forceinline__ void load_tile(const WindowParams &p, const TilePlace &at, Tile<KIND> &t) {
-  const int l = lane_id(), m = l & 15, a = l >> 4;
-  const int stride = PAGED && KIND != kCacheQ4 ? p.hkv : 1;
-  constexpr int kBytes = KIND == kCacheF32 ? 512 : (KIND == kCacheBf16 ? 256 : kQ4RowBytes);
-  const char *k = p.k + at.row0 * kBytes, *v = p.v + at.row0 * kBytes;
-  const int krow = (PAGED ? m : min(m, at.last)) * stride;
-  int vrow[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) vrow[r] = (PAGED ? 4 * a + r : min(4 * a + r, at.last)) * stride;
+// row0: the tile's first row, in units of rows.
+template <int KIND>
+__device__ __forceinline__ void load_tile(const WindowParams &p, int64_t row0, const Offsets<KIND> &o,
+                                          Tile<KIND> &t) {
+  const char *k = p.k + row0 * o.kBytes, *v = p.v + row0 * o.kBytes;
   if constexpr (KIND == kCacheBf16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + (uint32_t)(krow * 256 + 64 * i + 16 * a)));
+    for (int i = 0; i < 4; ++i) t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + o.k + 64 * i));
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      t.v[r] = __builtin_nontemporal_load((const u32x4 *)(v + (uint32_t)(vrow[r] * 256 + 16 * m)));
+    for (int r = 0; r < 4; ++r) t.v[r] = __builtin_nontemporal_load((const u32x4 *)(v + o.v[r]));
   } else if constexpr (KIND == kCacheF32) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + (uint32_t)(krow * 512 + 64 * i + 16 * a)));
+    for (int i = 0; i < 8; ++i) t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + o.k + 64 * i));
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        t.v[r][j] =
-            __builtin_nontemporal_load((const u32x4 *)(v + (uint32_t)(vrow[r] * 512 + 256 * j + 16 * m)));
+        t.v[r][j] = __builtin_nontemporal_load((const u32x4 *)(v + o.v[r] + 256 * j));
   } else {
-    const uint8_t *ks = p.ks + at.row0 * kQ4Scales, *vs = p.vs + at.row0 * kQ4Scales;
-    t.k = __builtin_nontemporal_load((const u32x4 *)(k + (uint32_t)(krow * kQ4RowBytes + 16 * a)));
-    t.ks = (uint32_t)ks[(uint32_t)(krow * kQ4Scales + a)];
-    if (PAGED) {  // the quarter's four rows of scales are one run
-      t.vs = *(const u32x4 *)(vs + (uint32_t)(16 * a));
-    } else {
+    const uint8_t *ks = p.ks + row0 * kQ4Scales, *vs = p.vs + row0 * kQ4Scales;
+    t.k = __builtin_nontemporal_load((const u32x4 *)(k + o.k));
+    t.ks = (uint32_t)ks[o.ks];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) t.vs[r] = *(const uint32_t *)(vs + (uint32_t)(vrow[r] * kQ4Scales));
+    for (int r = 0; r < 4; ++r) {
+      t.v[r] = __builtin_nontemporal_load((const uint32_t *)(v + o.v[r]));
+      t.vs[r] = *(const uint32_t *)(vs + o.vs[r]);
     }
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      t.v[r] = __builtin_nontemporal_load((const uint32_t *)(v + (uint32_t)(vrow[r] * kQ4RowBytes + 4 * m)));
   }
 }
 
@@ -234,10 +237,12 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
           x[4 + r][d] = tb.v[r][d];
         }
       } else {
-        const int sh = 8 * ((lane_id() & 15) >> 2);
+        // (the group's scale byte rotated to where a float has its exponent;
+        // the conversion looks at nothing else)
+        const uint32_t sh = (8 * ((lane_id() & 15) >> 2) + 9) & 31;
         const uint32_t sa = ta.vs[r], sb = tb.vs[r];
-        q4_values(ta.v[r], __uint_as_float((sa >> sh & 255u) << 23), x[r]);
-        q4_values(tb.v[r], __uint_as_float((sb >> sh & 255u) << 23), x[4 + r]);
+        q4_values(ta.v[r], __uint_as_float(__builtin_amdgcn_alignbit(sa, sa, sh)), x[r]);
+        q4_values(tb.v[r], __uint_as_float(__builtin_amdgcn_alignbit(sb, sb, sh)), x[4 + r]);
       }
     }
 #pragma unroll
@@ -265,16 +270,25 @@ __device__ __forceinline__ void store_out(const WindowParams &p, int64_t at, flo
   else ((uint16_t *)p.out)[at] = f32_to_bf16_rne(x);
 }
 
-// grid: splits fastest, then KV heads, then sequences.  The waves of a
+// Splits of a (sequence, KV head) that are done; 0 between calls.  Only calls
+// of fewer items than kSplitItems split.
+constexpr int kSplitItems = 512;
+static __device__ uint32_t splits_done[kSplitItems];
+
+// grid: splits fastest, then KV heads, then sequences; where a position holds
+// the rows of all heads, the heads fastest, so that they are read at about the
+// same time.  The waves of a
 // workgroup take the steps of two tiles in turn, each with the loads of its
 // next step under way while it computes.
 template <int KIND, bool PAGED, int NW>
 __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_attend(WindowParams p) {
+  constexpr int kAhead = KIND == kCacheQ4 ? 2 : 1;   // steps under way beside the computed one
   extern __shared__ float lds[];
-  uint32_t i0 = blockIdx.x;
-  const int s = (int)(i0 % (uint32_t)p.nsplit);
-  i0 /= (uint32_t)p.nsplit;
-  const int g = (int)(i0 % (uint32_t)p.hkv), b = (int)(i0 / (uint32_t)p.hkv);
+  constexpr bool kInside = PAGED && KIND != kCacheQ4;   // the heads lie inside a position
+  const uint32_t n0 = kInside ? p.hkv : p.nsplit, n1 = kInside ? p.nsplit : p.hkv;
+  const uint32_t x0 = blockIdx.x % n0, x1 = blockIdx.x / n0;
+  const int b = (int)(x1 / n1);
+  const int s = (int)(kInside ? x1 % n1 : x0), g = (int)(kInside ? x0 : x1 % n1);
   const int L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, b, p.ncap));
   const TileRange tr = tile_range(L, p.n_sink, p.window);
   const int nsp = (tr.n + p.span - 1) / p.span;  // splits of this sequence
@@ -291,6 +305,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
 
   QRegs<KIND> qr;
   load_query<KIND>(p, b, g, qr);
+  const Offsets<KIND> offs(PAGED && KIND != kCacheQ4 ? p.hkv : 1, kTile - 1);
 
   float m = kFloor, ls = 0.f;  // of this lane's head; ls over its own positions
   f32x4 acc[8];
@@ -325,19 +340,18 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     for (int u = 0; u < 2; ++u) {
       const int t = tile_of(i, u);
       st.ok[u] = t < t1;
-      TilePlace at;
       if (PAGED) {
         const int slot = 2 * (i & 31) + u;
         st.ok[u] = st.ok[u] && !(outside >> slot & 1);
         const int64_t page = __builtin_amdgcn_readlane(pages, slot);
-        at.row0 = KIND == kCacheQ4 ? (page * p.hkv + g) * kTile : page * kTile * p.hkv + g;
-        at.last = kTile - 1;
+        load_tile<KIND>(p, KIND == kCacheQ4 ? (page * p.hkv + g) * kTile : page * kTile * p.hkv + g,
+                        offs, st.tile[u]);
       } else {
-        const int first = st.ok[u] ? tr.tile(t) * kTile : 0;
-        at.row0 = ((int64_t)b * p.hkv + g) * p.ncap + first;
-        at.last = min(kTile - 1, L - 1 - first);
+        const int first = st.ok[u] ? tr.tile(t) * kTile : 0, last = L - 1 - first;
+        const int64_t row0 = ((int64_t)b * p.hkv + g) * p.ncap + first;
+        if (last >= kTile - 1) load_tile<KIND>(p, row0, offs, st.tile[u]);
+        else load_tile<KIND>(p, row0, Offsets<KIND>(1, last), st.tile[u]);
       }
-      load_tile<KIND, PAGED>(p, at, st.tile[u]);
     }
   };
   auto compute = [&](int i, Step &st) {
@@ -353,7 +367,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
       if (!whole) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int j = j0 + 4 * a + r;
+          const int j = j0 + 4 * r + a;
           const bool sees = st.ok[u] & (j < L) & ((j < tr.ns) | (j >= tr.lo));
           if (!sees) {
             z[u][r] = -__builtin_inff();
@@ -387,20 +401,23 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     add_values<KIND>(acc, st.tile[0], st.tile[1], pw[0], pw[1]);
   };
 
-  Step sa, sb;
-  if (steps > 0) {
-    hold_pages(0);
-    load(0, sa);
-  }
-  for (int i = 0; i < steps; i += 2) {   // (an even number of steps between two sets of pages)
-    if (i + 1 < steps) load(i + 1, sb);
-    compute(i, sa);
-    if (i + 1 >= steps) break;
-    if (i + 2 < steps) {
-      hold_pages(i + 2);
-      load(i + 2, sa);
+  Step st[kAhead + 1];
+#pragma unroll
+  for (int d = 0; d < kAhead; ++d)
+    if (d < steps) {
+      hold_pages(d);
+      load(d, st[d]);
     }
-    compute(i + 1, sb);
+  for (int i = 0; i < steps; i += kAhead + 1) {
+#pragma unroll
+    for (int d = 0; d <= kAhead; ++d) {
+      if (i + d >= steps) break;
+      if (i + d + kAhead < steps) {
+        hold_pages(i + d + kAhead);
+        load(i + d + kAhead, st[(d + kAhead) % (kAhead + 1)]);
+      }
+      compute(i + d, st[d]);
+    }
   }
 
   // Join the waves: per head a common maximum, scaled sums and outputs.
@@ -441,83 +458,72 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     } else {
       float *pp = p.part + ((orow + hh) * p.nsplit + s) * kPartStride;
       if (c == 0) {
-        pp[0] = M;
-        pp[1] = sum;
+        put_shared(pp, M);
+        put_shared(pp + 1, sum);
       }
-      pp[2 + c] = v;
+      put_shared(pp + 2 + c, v);
     }
   }
-}
+  if (nsp == 1) return;
 
-// Joins the splits of each query head, one wave each; sequences of one split
-// are done already.
-template <int KIND>
-__global__ __launch_bounds__(64 * kMergeWaves) void k_token_merge(WindowParams p) {
-  const int row = (int)blockIdx.x * kMergeWaves + __builtin_amdgcn_readfirstlane(wave_id());
-  if (row >= p.batch * p.hq) return;
-  const TileRange tr =
-      tile_range(clamp_len(p.seq_lens, row / p.hq, p.ncap), p.n_sink, p.window);
-  const int nsp = (tr.n + p.span - 1) / p.span;
-  if (nsp <= 1) return;
-  const Joined v = join_splits(p.part + (int64_t)row * p.nsplit * kPartStride, nsp);
-  const int64_t at = (int64_t)row * kHeadDim + 2 * lane_id();
-  store_out<KIND>(p, at, v.x);
-  store_out<KIND>(p, at + 1, v.y);
+  // The workgroup that finishes last joins the splits, a wave per query head.
+  // Each one counts itself once its partials have arrived where every compute
+  // unit sees them (which fences would ensure too, by writing back and
+  // emptying the L2 caches: 5 us more); the count wraps to 0 with the last,
+  // ready for the next call.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    *(uint32_t *)lds = atomicInc(&splits_done[b * p.hkv + g], (uint32_t)nsp - 1);
+  __syncthreads();
+  if (*(volatile uint32_t *)lds != (uint32_t)nsp - 1) return;
+  for (int hh = w; hh < p.G; hh += NW) {
+    const Joined v = join_splits<true>(p.part + (orow + hh) * p.nsplit * kPartStride, nsp);
+    const int64_t at = (orow + hh) * kHeadDim + 2 * l;
+    store_out<KIND>(p, at, v.x);
+    store_out<KIND>(p, at + 1, v.y);
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-// Waves of a workgroup: eight; four where the heads' outputs of eight would not
-// leave LDS for a second workgroup (more than eight heads to a KV head), and
-// for float32, whose two steps in registers leave room for one wave per SIMD.
-static int token_waves(const WindowParams &p, int kind) {
-  return p.G <= 8 && kind != kCacheF32 ? 8 : 4;
-}
+// Waves of a workgroup: eight, so that one fills a compute unit; four for
+// float32, whose two steps in registers leave room for one wave per SIMD.
+static constexpr int token_waves(int kind) { return kind == kCacheF32 ? 4 : 8; }
 
 void window_split(WindowParams &p, int kind) {
-  const int waves = token_waves(p, kind);
+  const int waves = token_waves(kind);
   const int64_t cap = (p.ncap + kTile - 1) / kTile;
   int64_t tiles = ((int64_t)p.n_sink + kTile - 1) / kTile + ((int64_t)p.window + kTile - 1) / kTile + 1;
   if (tiles > cap) tiles = cap;
   if (tiles < 1) tiles = 1;
   const int64_t items = (int64_t)p.batch * p.hkv;
   const int64_t step = 2 * waves;
-  const int64_t target = 4 * kUnits * 4 / waves;
+  const int64_t target = 2 * kUnits * 4 / waves;
   int64_t split = items > 0 ? (target + items - 1) / items : 1;
-  const int64_t most = (tiles + step * kStepsMin - 1) / (step * kStepsMin);
-  split = split < 1 ? 1 : (split > most ? most : split);
+  const int64_t most = (tiles + step - 1) / step;   // at least a step for each wave
+  split = split < 1 || items > kSplitItems ? 1 : (split > most ? most : split);
   int64_t span = (tiles + split - 1) / split;
   span = (span + step - 1) / step * step;
   p.span = (int32_t)span;
   p.nsplit = (int32_t)((tiles + span - 1) / span);
 }
 
-template <int KIND, bool PAGED, int NW>
+template <int KIND, bool PAGED>
 static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
+  constexpr int NW = token_waves(KIND);
   const int64_t grid = (int64_t)p.batch * p.hkv * p.nsplit;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   k_token_attend<KIND, PAGED, NW><<<(unsigned)grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.nsplit == 1) return e;
-  const unsigned rows = (unsigned)(p.batch * p.hq);
-  k_token_merge<KIND><<<(rows + kMergeWaves - 1) / kMergeWaves, 64 * kMergeWaves, 0, st>>>(p);
   return hipGetLastError();
-}
-
-template <int KIND>
-static hipError_t launch_token_kind(const WindowParams &p, bool paged, hipStream_t st) {
-  if constexpr (KIND != kCacheF32)
-    if (token_waves(p, KIND) == 8)
-      return paged ? launch_token<KIND, true, 8>(p, st) : launch_token<KIND, false, 8>(p, st);
-  return paged ? launch_token<KIND, true, 4>(p, st) : launch_token<KIND, false, 4>(p, st);
 }
 
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
   switch (kind) {
-    case kCacheF32: return launch_token_kind<kCacheF32>(p, paged, st);
-    case kCacheBf16: return launch_token_kind<kCacheBf16>(p, paged, st);
-    default: return launch_token_kind<kCacheQ4>(p, paged, st);
+    case kCacheF32: return paged ? launch_token<kCacheF32, true>(p, st) : launch_token<kCacheF32, false>(p, st);
+    case kCacheBf16: return paged ? launch_token<kCacheBf16, true>(p, st) : launch_token<kCacheBf16, false>(p, st);
+    default: return paged ? launch_token<kCacheQ4, true>(p, st) : launch_token<kCacheQ4, false>(p, st);
   }
 }
 

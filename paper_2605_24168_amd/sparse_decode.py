@@ -714,8 +714,16 @@ def _q4_descs(cache: Q4Cache) -> tuple:
                                              ("v", cache.v, cache.v_scales)))
 
 
+def _empty_like(q: torch.Tensor, stream) -> torch.Tensor:
+    if stream is None and q.is_contiguous():
+        return torch.empty_like(q)
+    return _empty(q.shape, q.dtype, q.device, stream)
+
+
 def _need_vector(t: torch.Tensor, name: str, n: Optional[int] = None) -> None:
-    _need_device(t, name, torch.int32)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.int32 or \
+            not t.is_contiguous():
+        _need_device(t, name, torch.int32)  # raises
     if t.dim() != 1 or (n is not None and t.shape[0] != n):
         raise ValueError(f"{name} must have the shape [{'n' if n is None else n}]")
 
@@ -733,25 +741,31 @@ def _batch_of(cache, seq_lens, starts) -> int:
 
 
 def _same_device(first: torch.Tensor, *others) -> None:
+    index = first.get_device()
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"tensors on {first.device} and {t.device}")
 
 
-def _call(fn: str, device, stream, *args) -> None:
-    """One library call on `device`, with the stream appended."""
-    if device.index == torch._C._cuda_getDevice():
-        status = getattr(_raw, fn)(*args, _stream(stream))
+def _call(fn, index: int, stream, *args) -> None:
+    """One library call on device `index`, with the stream appended."""
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, _stream(stream))
     else:
-        with torch.cuda.device(device):
-            status = getattr(_raw, fn)(*args, _stream(stream))
-    _check(status, fn)
+        with torch.cuda.device(index):
+            status = fn(*args, _stream(stream))
+    if status != SD_OK:
+        _check(status, fn.__name__)
 
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
-    """An output, from the memory of the stream that the call runs on."""
+    """An output, from the memory of the stream that the call runs on (on the
+    device's current stream without one)."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if device.index == torch._C._cuda_getDevice():
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.device(device):
+            return torch.empty(shape, dtype=dtype, device=device)
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(_stream(stream), device=device)
     with torch.cuda.stream(stream):
@@ -767,10 +781,10 @@ def sparse_decode_window_attention(q, cache: KVCache, seq_lens, window: Window, 
     are left as they are in `out` (unset without one)."""
     batch = _batch_of(cache, seq_lens, q_starts)
     if out is None:
-        out = _empty(q.shape, q.dtype, q.device, stream)
+        out = _empty_like(q, stream)
     _same_device(q, cache.k, cache.v, cache.block_table, seq_lens, q_starts, out)
     cq, (kk, kv), co = _desc(q, "q"), _kv_desc(cache, "k", "v"), _desc(out, "out")
-    _call("sparse_decode_window_attention", q.device, stream, cq, kk, kv, seq_lens.data_ptr(),
+    _call(_raw.sparse_decode_window_attention, q.get_device(), stream, cq, kk, kv, seq_lens.data_ptr(),
           q_starts.data_ptr() if q_starts is not None else None, batch, _window_desc(window), co)
     return out
 
@@ -792,7 +806,7 @@ def sparse_decode_q4_append(k, v, cache: Q4Cache, seq_lens, starts=None, stream=
     batch = _batch_of(cache, seq_lens, starts)
     _same_device(k, v, *cache.pools, cache.block_table, seq_lens, starts)
     ck, cv, (kk, kv) = _desc(k, "k"), _desc(v, "v"), _q4_descs(cache)
-    _call("sparse_decode_q4_append", k.device, stream, ck, cv, kk, kv, seq_lens.data_ptr(),
+    _call(_raw.sparse_decode_q4_append, k.get_device(), stream, ck, cv, kk, kv, seq_lens.data_ptr(),
           starts.data_ptr() if starts is not None else None, batch)
 
 
@@ -813,7 +827,7 @@ def sparse_decode_q4_load(cache: Q4Cache, seq_lens, starts=None, tokens: Optiona
     v = _empty(shape, dtype, dev, stream) if v is None else v
     _same_device(k, v, *cache.pools, cache.block_table, seq_lens, starts)
     ck, cv, (kk, kv) = _desc(k, "k"), _desc(v, "v"), _q4_descs(cache)
-    _call("sparse_decode_q4_load", k.device, stream, kk, kv, seq_lens.data_ptr(),
+    _call(_raw.sparse_decode_q4_load, k.get_device(), stream, kk, kv, seq_lens.data_ptr(),
           starts.data_ptr() if starts is not None else None, batch, ck, cv)
     return k, v
 
@@ -826,11 +840,11 @@ def sparse_decode_q4_attention(q, cache: Q4Cache, seq_lens, window: Optional[Win
     if q.shape[0] != seq_lens.shape[0]:
         raise ValueError("q and seq_lens must have the same number of sequences")
     if out is None:
-        out = _empty(q.shape, q.dtype, q.device, stream)
+        out = _empty_like(q, stream)
     _same_device(q, *cache.pools, cache.block_table, seq_lens, out)
     cq, (kk, kv), co = _desc(q, "q"), _q4_descs(cache), _desc(out, "out")
     cw = _window_desc(window) if window is not None else None
-    _call("sparse_decode_q4_attention", q.device, stream, cq, kk, kv, seq_lens.data_ptr(), cw, co)
+    _call(_raw.sparse_decode_q4_attention, q.get_device(), stream, cq, kk, kv, seq_lens.data_ptr(), cw, co)
     return out
 
 
@@ -871,7 +885,7 @@ def sparse_decode_pages_extend(pages: Pages, grow, status=None, stream=None):
     status = _empty((batch,), torch.int32, dev, stream) if status is None else status
     _need_vector(status, "status", batch)
     _same_device(pages.block_table, grow, status)
-    _call("sparse_decode_pages_extend", dev, stream, cp, grow.data_ptr(), status.data_ptr())
+    _call(_raw.sparse_decode_pages_extend, dev.index, stream, cp, grow.data_ptr(), status.data_ptr())
     return status
 
 
@@ -888,7 +902,7 @@ def sparse_decode_pages_fork(pages: Pages, to: Pages, parents, pools: Sequence[t
     _need_vector(status, "status", batch)
     _same_device(pages.block_table, to.block_table, parents, status)
     pl, n = _pools_desc(pools, dev)
-    _call("sparse_decode_pages_fork", dev, stream, cp, ct, parents.data_ptr(), int(bool(keep)), pl,
+    _call(_raw.sparse_decode_pages_fork, dev.index, stream, cp, ct, parents.data_ptr(), int(bool(keep)), pl,
           n, status.data_ptr())
     return status
 
@@ -898,7 +912,7 @@ def sparse_decode_pages_free(pages: Pages, rows, stream=None) -> None:
     cp = _pages_desc(pages)
     _need_vector(rows, "rows")
     _same_device(pages.block_table, rows)
-    _call("sparse_decode_pages_free", rows.device, stream, cp, rows.data_ptr(), rows.shape[0])
+    _call(_raw.sparse_decode_pages_free, rows.get_device(), stream, cp, rows.data_ptr(), rows.shape[0])
 
 
 def sparse_decode_pages_copy(pools: Sequence[torch.Tensor], src, dst, stream=None) -> None:
@@ -908,7 +922,7 @@ def sparse_decode_pages_copy(pools: Sequence[torch.Tensor], src, dst, stream=Non
     _need_vector(dst, "dst", int(src.shape[0]))
     _same_device(src, dst)
     pl, n = _pools_desc(pools, src.device)
-    _call("sparse_decode_pages_copy", src.device, stream, pl, n, src.data_ptr(), dst.data_ptr(),
+    _call(_raw.sparse_decode_pages_copy, src.get_device(), stream, pl, n, src.data_ptr(), dst.data_ptr(),
           src.shape[0])
 
 
@@ -925,7 +939,7 @@ def sparse_decode_pages_compact(pages: Pages, pools: Sequence[torch.Tensor] = ()
     _need_vector(n_live, "n_live", 1)
     _same_device(pages.block_table, remap, n_live)
     pl, count = _pools_desc(pools, dev)
-    _call("sparse_decode_pages_compact", dev, stream, cp, pl, count, remap.data_ptr(),
+    _call(_raw.sparse_decode_pages_compact, dev.index, stream, cp, pl, count, remap.data_ptr(),
           n_live.data_ptr())
     return remap, n_live
 

@@ -260,7 +260,8 @@ def test_workspace_sizes():
     assert rc == 0 and long_ > 0
     rc, local = size(tensor((2, 32, 128)), kv((2, 8, 131072, 128)), 2, 0, sd.SdWindow(4, 1020, 0.0))
     assert rc == 0 and local <= long_
-    assert size(tensor((500, 32, 128)), kv(), 2, 1, every) == (0, 0)   # chunks need none
+    assert size(tensor((50000, 32, 128)), kv(), 2, 1, every) == (0, 0)  # many rows: no splits
+    assert size(tensor((8, 32, 128)), kv((2, 8, 131072, 128)), 2, 1, every)[1] > 0
     assert size(tensor((3, 32, 128)), kv(), 2, 0, every)[0] == INVALID
     assert sd.lib.sparse_decode_window_workspace_size(ref(tensor((2, 32, 128))), ref(kv()), 2, 0,
                                                       ref(every), None) == INVALID
