@@ -12,39 +12,51 @@
 namespace sd {
 
 constexpr int kQ4Rows = kBlock / 16;  // rows of a workgroup at once
-constexpr int kQ4Unroll = 4;          // rows of a 16-lane group
+// Rows of a 16-lane group.  A group with more rows has more bytes under way,
+// but scatters its workgroup's writes in time: 250K positions of 8 heads take
+// 261, 246, 242 and 253 us to append with 1, 2, 4 and 8 rows (contiguous
+// caches 233, 235, 242, 242), and 250, 289, 290 and 293 us to load.
+constexpr int kAppendRows = 2, kLoadRows = 1;
 
 // Where packed row t lives: its sequence and position, or b < 0 for a row of
-// no sequence.
+// no sequence.  (T * Hkv rows fit in 31 bits.)
 struct TokenPlace {
   int b;
-  int64_t j;
+  int j;
 };
 
-__device__ __forceinline__ TokenPlace token_place(const Q4Params &p, int64_t t) {
-  TokenPlace r;
-  int64_t first = t, n = 1;
-  r.b = (int)t;
-  r.j = -1;
+// The packed rows [first, next) of a sequence, whose first one is at position
+// j0 (below 0: before the sequence).
+struct TokenRun {
+  int b, first, next, j0;
+  __device__ __forceinline__ bool holds(int t) const { return t >= first && t < next; }
+};
+
+// The run that row t is in; b < 0 and empty if it is in none.
+__device__ __forceinline__ TokenRun token_run(const Q4Params &p, int t) {
+  TokenRun r{t, t, t + 1, 0};
   if (p.starts) {  // the last sequence that starts at or before t
-    int lo = 0, hi = p.batch;  // starts[lo - 1] <= t < starts[hi + 1], if they are ascending
+    int lo = 0, hi = p.batch;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (p.starts[mid] <= t) lo = mid + 1;
       else hi = mid;
     }
     r.b = lo - 1;
-    if (r.b < 0) return r;
-    first = clamp_start(p.starts, r.b, p.n_rows);
-    n = clamp_start(p.starts, r.b + 1, p.n_rows) - first;
-    if (t - first >= n) {
-      r.b = -1;
-      return r;
-    }
+    if (r.b < 0) return TokenRun{-1, 0, 0, 0};
+    r.first = (int)clamp_start(p.starts, r.b, p.n_rows);
+    r.next = (int)clamp_start(p.starts, r.b + 1, p.n_rows);
+    if (!r.holds(t)) return TokenRun{-1, 0, 0, 0};
   }
-  const int L = clamp_len(p.seq_lens, r.b, p.ncap);
-  r.j = L - n + (t - first);
+  r.j0 = clamp_len(p.seq_lens, r.b, p.ncap) - (r.next - r.first);
   return r;
+}
+
+// Row t's place; run: of the workgroup's first row, which most rows share.
+__device__ __forceinline__ TokenPlace token_place(const Q4Params &p, const TokenRun &run, int t) {
+  if (run.holds(t)) return TokenPlace{run.b, run.j0 + (t - run.first)};
+  const TokenRun r = token_run(p, t);
+  return TokenPlace{r.b, r.j0 + (t - r.first)};
 }
 
 // Row index in the cache of position j of sequence b, or -1.
@@ -79,81 +91,125 @@ __device__ __forceinline__ void q4_encode(const float x[8], uint32_t &codes, uin
   if (scale == (uint32_t)kQ4NanScale) codes = 0;
 }
 
+// Eight channels of a row as they lie in memory, and as floats.
 template <bool BF16>
-__device__ __forceinline__ void load_channels(const void *base, int64_t row, int c, float x[8]) {
-  if (BF16) {
-    const u32x4 w = __builtin_nontemporal_load((const u32x4 *)((const uint16_t *)base + row * kHeadDim + 8 * c));
+struct Channels {
+  u32x4 w[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void *base, int64_t row, int c) {
+    const u32x4 *src = BF16 ? (const u32x4 *)((const uint16_t *)base + row * kHeadDim + 8 * c)
+                            : (const u32x4 *)((const float *)base + row * kHeadDim + 8 * c);
+#pragma unroll
+    for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = __builtin_nontemporal_load(src + i);
+  }
+  __device__ __forceinline__ void floats(float x[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t y = w[i];
-      x[2 * i] = bf16_to_f32(y & 0xFFFFu);
-      x[2 * i + 1] = __uint_as_float(y & 0xFFFF0000u);
-    }
-  } else {
-    const f32x4 *src = (const f32x4 *)((const float *)base + row * kHeadDim + 8 * c);
-    const f32x4 u = __builtin_nontemporal_load(src), v = __builtin_nontemporal_load(src + 1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = u[i];
-      x[4 + i] = v[i];
+      if constexpr (BF16) {
+        const uint32_t y = w[0][i];
+        x[2 * i] = bf16_to_f32(y & 0xFFFFu);
+        x[2 * i + 1] = __uint_as_float(y & 0xFFFF0000u);
+      } else {
+        const uint32_t y = w[0][i], z = w[1][i];
+        x[i] = __uint_as_float(y);
+        x[4 + i] = __uint_as_float(z);
+      }
     }
   }
+};
+
+// Rows of this workgroup: U per 16-lane group, kQ4Rows apart, so that the
+// workgroup's are one run.
+template <int U>
+__device__ __forceinline__ int first_row() {
+  return (int)blockIdx.x * U * kQ4Rows;
 }
 
+template <int U, bool PAGED>
+__device__ __forceinline__ int64_t group_row(const Q4Params &p, const TokenRun &run, int u, int &r,
+                                             TokenPlace &tp) {
+  r = first_row<U>() + u * kQ4Rows + (int)(threadIdx.x >> 4);
+  if (r >= (int)(p.n_rows * p.hkv)) {
+    r = -1;
+    return -1;
+  }
+  tp = token_place(p, run, (int)((uint32_t)r / (uint32_t)p.hkv));
+  return q4_row<PAGED>(p, tp, (int)((uint32_t)r % (uint32_t)p.hkv));
+}
+
+// The rows' loads are under way before their places are looked up.
 template <bool BF16, bool PAGED>
 __global__ __launch_bounds__(kBlock) void k_q4_append(Q4Params p) {
-  const int64_t rows = p.n_rows * p.hkv;
+  const int rows = (int)(p.n_rows * p.hkv);
   const int c = threadIdx.x & 15;
-#pragma unroll 1
-  for (int u = 0; u < kQ4Unroll; ++u) {
-    const int64_t r = ((int64_t)blockIdx.x * kQ4Unroll + u) * kQ4Rows + (threadIdx.x >> 4);
-    if (r >= rows) return;  // (a row's sixteen lanes leave together)
-    const int64_t t = r / p.hkv;
-    const int64_t at = q4_row<PAGED>(p, token_place(p, t), (int)(r % p.hkv));
-    if (at < 0) continue;
+  Channels<BF16> x[kAppendRows][2];
+#pragma unroll
+  for (int u = 0; u < kAppendRows; ++u) {
+    const int r = first_row<kAppendRows>() + u * kQ4Rows + (int)(threadIdx.x >> 4);
+    x[u][0].load(p.xk, min(r, rows - 1), c);
+    x[u][1].load(p.xv, min(r, rows - 1), c);
+  }
+  const TokenRun run = token_run(p, (int)((uint32_t)first_row<kAppendRows>() / (uint32_t)p.hkv));
+#pragma unroll
+  for (int u = 0; u < kAppendRows; ++u) {
+    int r;
+    TokenPlace tp;
+    const int64_t at = group_row<kAppendRows, PAGED>(p, run, u, r, tp);
+    if (at < 0) continue;  // (a row's sixteen lanes together)
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      float x[8];
-      load_channels<BF16>(w ? p.xv : p.xk, r, c, x);
+      float y[8];
+      x[u][w].floats(y);
       uint32_t codes, scale;
-      q4_encode(x, codes, scale);
+      q4_encode(y, codes, scale);
+      // The row's four scale bytes in its first lane.
+      scale <<= 8 * (c >> 2);
+      scale |= (uint32_t)__shfl_xor((int)scale, 4);
+      scale |= (uint32_t)__shfl_xor((int)scale, 8);
       *(uint32_t *)((w ? p.v : p.k) + at * kQ4RowBytes + 4 * c) = codes;
-      if ((c & 3) == 0) (w ? p.vs : p.ks)[at * kQ4Scales + (c >> 2)] = (uint8_t)scale;
+      if (c == 0) *(uint32_t *)((w ? p.vs : p.ks) + at * kQ4Scales) = scale;
     }
   }
 }
 
 template <bool BF16, bool PAGED>
 __global__ __launch_bounds__(kBlock) void k_q4_load(Q4Params p) {
-  const int64_t rows = p.n_rows * p.hkv;
   const int c = threadIdx.x & 15;
-#pragma unroll 1
-  for (int u = 0; u < kQ4Unroll; ++u) {
-    const int64_t r = ((int64_t)blockIdx.x * kQ4Unroll + u) * kQ4Rows + (threadIdx.x >> 4);
-    if (r >= rows) return;
-    const TokenPlace tp = token_place(p, r / p.hkv);
-    if (tp.b < 0) continue;
-    const int64_t at = q4_row<PAGED>(p, tp, (int)(r % p.hkv));
+  const TokenRun run = token_run(p, (int)((uint32_t)first_row<kLoadRows>() / (uint32_t)p.hkv));
+  int r[kLoadRows];
+  uint32_t codes[kLoadRows][2], scale[kLoadRows][2];
+#pragma unroll
+  for (int u = 0; u < kLoadRows; ++u) {
+    TokenPlace tp;
+    const int64_t at = group_row<kLoadRows, PAGED>(p, run, u, r[u], tp);
+    if (r[u] >= 0 && tp.b < 0) r[u] = -1;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      u32x4 y = {0u, 0u, 0u, 0u};
-      if (at >= 0) {
-        const uint32_t codes = *(const uint32_t *)((w ? p.v : p.k) + at * kQ4RowBytes + 4 * c);
-        const uint32_t scale = (w ? p.vs : p.ks)[at * kQ4Scales + (c >> 2)];
-        const float f = __uint_as_float(scale << 23);
-        y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f, 0));
-        y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f, 1));
-        y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f, 2));
-        y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f, 3));
-      }
+      codes[u][w] = scale[u][w] = 0u;
+      if (at < 0) continue;
+      codes[u][w] = *(const uint32_t *)((w ? p.v : p.k) + at * kQ4RowBytes + 4 * c);
+      scale[u][w] = (w ? p.vs : p.ks)[at * kQ4Scales + (c >> 2)];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kLoadRows; ++u) {
+    if (r[u] < 0) continue;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const float f = __uint_as_float(scale[u][w] << 23);
+      u32x4 y;
+      y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[u][w], f, 0));
+      y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[u][w], f, 1));
+      y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[u][w], f, 2));
+      y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[u][w], f, 3));
+      const int64_t at = (int64_t)r[u] * kHeadDim + 8 * c;
       if (BF16) {
-        *(u32x4 *)((uint16_t *)(w ? p.xv : p.xk) + r * kHeadDim + 8 * c) = y;
+        __builtin_nontemporal_store(y, (u32x4 *)((uint16_t *)(w ? p.xv : p.xk) + at));
       } else {
-        u32x4 *dst = (u32x4 *)((float *)(w ? p.xv : p.xk) + r * kHeadDim + 8 * c);
+        u32x4 *dst = (u32x4 *)((float *)(w ? p.xv : p.xk) + at);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const uint32_t a = y[2 * i], b = y[2 * i + 1];
-          dst[i] = u32x4{a << 16, a & 0xFFFF0000u, b << 16, b & 0xFFFF0000u};
+          __builtin_nontemporal_store(u32x4{a << 16, a & 0xFFFF0000u, b << 16, b & 0xFFFF0000u}, dst + i);
         }
       }
     }
@@ -162,7 +218,7 @@ __global__ __launch_bounds__(kBlock) void k_q4_load(Q4Params p) {
 
 template <bool APPEND>
 static hipError_t launch_q4(const Q4Params &p, bool bf16, bool paged, hipStream_t st) {
-  const int64_t per = kQ4Rows * kQ4Unroll;
+  const int64_t per = kQ4Rows * (APPEND ? kAppendRows : kLoadRows);
   const int64_t grid = (p.n_rows * p.hkv + per - 1) / per;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   if (grid == 0) return hipSuccess;
