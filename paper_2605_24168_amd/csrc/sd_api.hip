@@ -1245,9 +1245,9 @@ sd::WindowParams window_params(const CacheShape &c, int64_t batch, int64_t rows,
 
 // Splits of a call (one query per sequence, or packed ones) and the bytes of
 // its partials.
-size_t window_work(sd::WindowParams &p, int kind, bool packed) {
+size_t window_work(sd::WindowParams &p, int kind, bool paged, bool packed) {
   if (packed) sd::chunk_split(p, kind);
-  else sd::window_split(p, kind);
+  else sd::window_split(p, kind, paged);
   if (p.nsplit <= 1) return 0;
   return align_up((size_t)p.n_rows * p.hq * p.nsplit * sd::kPartStride * sizeof(float));
 }
@@ -1273,7 +1273,7 @@ sd_status check_window_call(const sd_tensor *q, const sd_kv *K, int64_t batch, b
 // Splits, scratch and launches of a call.
 sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
   const bool packed = p.q_starts != nullptr;
-  const size_t bytes = window_work(p, kind, packed);
+  const size_t bytes = window_work(p, kind, paged, packed);
   std::lock_guard<std::mutex> lk(g_mu);
   if (bytes) {
     DevState *ds = nullptr;
@@ -1298,7 +1298,8 @@ sd_status sparse_decode_window_workspace_size(const sd_tensor *q, const sd_kv *K
   const sd_status st = check_window_call(q, K, batch, packed != 0, w, c, rows, hq);
   if (st) return st;
   sd::WindowParams p = window_params(c, batch, rows, hq, w);
-  *bytes = window_work(p, q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16, packed != 0);
+  *bytes = window_work(p, q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16, c.paged,
+                       packed != 0);
   return SD_OK;
 }
 
@@ -1346,7 +1347,7 @@ sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K, c
   if (hq % c.hkv) return SD_ERR_INVALID_ARG;
   if (hq / c.hkv > sd::kMaxGroup) return SD_ERR_UNSUPPORTED;
   sd::WindowParams p = window_params(c, rows, rows, hq, w);
-  *bytes = window_work(p, sd::kCacheQ4, false);
+  *bytes = window_work(p, sd::kCacheQ4, c.paged, false);
   return SD_OK;
 }
 

@@ -37,11 +37,12 @@ struct WindowParams {
   float scale2;                // softmax scale times log2(e)
   int32_t span;                // tiles of 16 positions per split
   int32_t nsplit;
+  int32_t quad;                // a workgroup takes four KV heads (one query per sequence)
 };
 
 // Splits of one sequence and KV head over workgroups, from what the host
-// knows (see window_split); fills p.span and p.nsplit.
-void window_split(WindowParams &p, int kind);
+// knows (see window_split); fills p.span, p.nsplit and p.quad.
+void window_split(WindowParams &p, int kind, bool paged);
 // The same for packed queries; fills p.nsplit.
 void chunk_split(WindowParams &p, int kind);
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);

@@ -277,31 +277,35 @@ static __device__ uint32_t splits_done[kSplitItems];
 
 // grid: splits fastest, then KV heads, then sequences; where a position holds
 // the rows of all heads, the heads fastest, so that they are read at about the
-// same time.  The waves of a
+// same time.  HEADS: KV heads of a workgroup, each with NW / HEADS waves.  The waves of a
 // workgroup take the steps of two tiles in turn, each with the loads of its
 // next step under way while it computes.
-template <int KIND, bool PAGED, int NW>
+template <int KIND, bool PAGED, int NW, int HEADS>
 __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_attend(WindowParams p) {
+  constexpr int NS = NW / HEADS;   // waves of a head
   constexpr int kAhead = KIND == kCacheQ4 ? 2 : 1;   // steps under way beside the computed one
   extern __shared__ float lds[];
   constexpr bool kInside = PAGED && KIND != kCacheQ4;   // the heads lie inside a position
-  const uint32_t n0 = kInside ? p.hkv : p.nsplit, n1 = kInside ? p.nsplit : p.hkv;
+  const int l = lane_id(), a = l >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(wave_id()), sub = w / HEADS;
+  const uint32_t groups = p.hkv / HEADS;
+  const uint32_t n0 = kInside ? groups : p.nsplit, n1 = kInside ? p.nsplit : groups;
   const uint32_t x0 = blockIdx.x % n0, x1 = blockIdx.x / n0;
   const int b = (int)(x1 / n1);
-  const int s = (int)(kInside ? x1 % n1 : x0), g = (int)(kInside ? x0 : x1 % n1);
+  const int s = (int)(kInside ? x1 % n1 : x0), g0 = HEADS * (int)(kInside ? x0 : x1 % n1);
+  const int g = g0 + w % HEADS;
   const int L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, b, p.ncap));
   const TileRange tr = tile_range(L, p.n_sink, p.window);
   const int nsp = (tr.n + p.span - 1) / p.span;  // splits of this sequence
   if (s > 0 && s >= nsp) return;
-  const int64_t orow = (int64_t)b * p.hq + (int64_t)g * p.G;
+  const int64_t orow = (int64_t)b * p.hq + (int64_t)g0 * p.G;   // of the workgroup's HEADS * G rows
+  const int orows = HEADS * p.G;
   if (nsp == 0) {
-    for (int i = threadIdx.x; i < p.G * kHeadDim; i += 64 * NW)
+    for (int i = threadIdx.x; i < orows * kHeadDim; i += 64 * NW)
       store_out<KIND>(p, orow * kHeadDim + i, 0.f);
     return;
   }
   const int t0 = s * p.span, t1 = min(tr.n, t0 + p.span);
-  const int l = lane_id(), a = l >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(wave_id());
 
   QRegs<KIND> qr;
   load_query<KIND>(p, b, g, qr);
@@ -315,8 +319,8 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   // Step i of this wave: tiles tile_of(i, 0) and the one after it.  Pages: 32
   // steps at a time, a tile per lane; outside: a bit for each that is not in
   // the pool.
-  auto tile_of = [&](int i, int u) { return t0 + 2 * (i * NW + w) + u; };
-  const int steps = t0 + 2 * w < t1 ? (t1 - t0 - 2 * w + 2 * NW - 1) / (2 * NW) : 0;
+  auto tile_of = [&](int i, int u) { return t0 + 2 * (i * NS + sub) + u; };
+  const int steps = t0 + 2 * sub < t1 ? (t1 - t0 - 2 * sub + 2 * NS - 1) / (2 * NS) : 0;
   int pages = 0;
   uint64_t outside = 0;
   auto hold_pages = [&](int i) {
@@ -441,17 +445,20 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
       }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < p.G * kHeadDim; i += 64 * NW) {
+  for (int i = threadIdx.x; i < orows * kHeadDim; i += 64 * NW) {
     const int hh = i / kHeadDim, c = i % kHeadDim;
+    // Row hh is head h of the workgroup's KV head q: in waves q, q + HEADS, ...
+    const int q = HEADS == 1 ? 0 : hh / p.G, h = HEADS == 1 ? hh : hh % p.G;
     float M = kFloor;
 #pragma unroll
-    for (int x = 0; x < NW; ++x) M = fmaxf(M, ml[2 * (x * p.G + hh)]);
+    for (int x = 0; x < NS; ++x) M = fmaxf(M, ml[2 * ((x * HEADS + q) * p.G + h)]);
     float sum = 0.f, v = 0.f;
 #pragma unroll
-    for (int x = 0; x < NW; ++x) {
-      const float f = __builtin_amdgcn_exp2f(ml[2 * (x * p.G + hh)] - M);
-      sum += f * ml[2 * (x * p.G + hh) + 1];
-      v += f * o[(x * p.G + hh) * kRow + c];
+    for (int x = 0; x < NS; ++x) {
+      const int row = (x * HEADS + q) * p.G + h;
+      const float f = __builtin_amdgcn_exp2f(ml[2 * row] - M);
+      sum += f * ml[2 * row + 1];
+      v += f * o[row * kRow + c];
     }
     if (nsp == 1) {
       store_out<KIND>(p, (orow + hh) * kHeadDim + c, sum > 0.f ? v / sum : 0.f);
@@ -474,10 +481,10 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0)
-    *(uint32_t *)lds = atomicInc(&splits_done[b * p.hkv + g], (uint32_t)nsp - 1);
+    *(uint32_t *)lds = atomicInc(&splits_done[x1 / n1 * groups + g0 / HEADS], (uint32_t)nsp - 1);
   __syncthreads();
   if (*(volatile uint32_t *)lds != (uint32_t)nsp - 1) return;
-  for (int hh = w; hh < p.G; hh += NW) {
+  for (int hh = w; hh < orows; hh += NW) {
     const Joined v = join_splits<true>(p.part + (orow + hh) * p.nsplit * kPartStride, nsp);
     const int64_t at = (orow + hh) * kHeadDim + 2 * l;
     store_out<KIND>(p, at, v.x);
@@ -492,14 +499,27 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
 // float32, whose two steps in registers leave room for one wave per SIMD.
 static constexpr int token_waves(int kind) { return kind == kCacheF32 ? 4 : 8; }
 
-void window_split(WindowParams &p, int kind) {
+// Four KV heads to a workgroup pay on bfloat16 pages, whose rows of one head
+// are scattered 256-byte pieces, once there is enough to read and few splits
+// are needed: 64 sequences of 200-64K with a window of 4096 take 177 us instead
+// of 196, 16 of 16K 169 instead of 190, 16 of 4K 49 instead of 53; below, the
+// longer joins cost more (16 of 1K: 20 instead of 19; 4 of 16K: 55 instead of
+// 53; one of 64K: 80 instead of 54).
+constexpr int64_t kQuadItems = 128;     // sequences times KV heads
+constexpr int64_t kQuadTiles = 32768;   // the same times tiles
+
+void window_split(WindowParams &p, int kind, bool paged) {
   const int waves = token_waves(kind);
   const int64_t cap = (p.ncap + kTile - 1) / kTile;
   int64_t tiles = ((int64_t)p.n_sink + kTile - 1) / kTile + ((int64_t)p.window + kTile - 1) / kTile + 1;
   if (tiles > cap) tiles = cap;
   if (tiles < 1) tiles = 1;
-  const int64_t items = (int64_t)p.batch * p.hkv;
-  const int64_t step = 2 * waves;
+  const int64_t all = (int64_t)p.batch * p.hkv;
+  p.quad = paged && kind == kCacheBf16 && p.hkv % 4 == 0 && all >= kQuadItems &&
+           all * tiles >= kQuadTiles;
+  const int heads = p.quad ? 4 : 1;
+  const int64_t items = all / heads;
+  const int64_t step = 2 * waves / heads;
   const int64_t target = 2 * kUnits * 4 / waves;
   int64_t split = items > 0 ? (target + items - 1) / items : 1;
   const int64_t most = (tiles + step - 1) / step;   // at least a step for each wave
@@ -510,20 +530,22 @@ void window_split(WindowParams &p, int kind) {
   p.nsplit = (int32_t)((tiles + span - 1) / span);
 }
 
-template <int KIND, bool PAGED>
+template <int KIND, bool PAGED, int HEADS>
 static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
   constexpr int NW = token_waves(KIND);
-  const int64_t grid = (int64_t)p.batch * p.hkv * p.nsplit;
+  const int64_t grid = (int64_t)p.batch * (p.hkv / HEADS) * p.nsplit;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_token_attend<KIND, PAGED, NW><<<(unsigned)grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
+  k_token_attend<KIND, PAGED, NW, HEADS>
+      <<<(unsigned)grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
   return hipGetLastError();
 }
 
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
+  if (p.quad) return launch_token<kCacheBf16, true, 4>(p, st);
   switch (kind) {
-    case kCacheF32: return paged ? launch_token<kCacheF32, true>(p, st) : launch_token<kCacheF32, false>(p, st);
-    case kCacheBf16: return paged ? launch_token<kCacheBf16, true>(p, st) : launch_token<kCacheBf16, false>(p, st);
-    default: return paged ? launch_token<kCacheQ4, true>(p, st) : launch_token<kCacheQ4, false>(p, st);
+    case kCacheF32: return paged ? launch_token<kCacheF32, true, 1>(p, st) : launch_token<kCacheF32, false, 1>(p, st);
+    case kCacheBf16: return paged ? launch_token<kCacheBf16, true, 1>(p, st) : launch_token<kCacheBf16, false, 1>(p, st);
+    default: return paged ? launch_token<kCacheQ4, true, 1>(p, st) : launch_token<kCacheQ4, false, 1>(p, st);
   }
 }
 

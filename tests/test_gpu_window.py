@@ -130,6 +130,18 @@ def test_long_sequences_split_over_workgroups(sd):
         pr.check(pr.run(sd.Window(100, 9000), False), 100, 9000)
 
 
+@pytest.mark.parametrize("hq,hkv", [(32, 8), (16, 16), (8, 4)])
+def test_many_sequences_on_pages(sd, hq, hkv):
+    # Enough sequences and positions for workgroups of four KV heads, whole
+    # and split.
+    B = 128 // hkv * 2
+    lens = [2100 + 61 * b % 900 for b in range(B)]
+    lens[1], lens[2], lens[3] = 0, 1, 33
+    pr = Problem(sd, lens, hq, hkv, "paged", "bf16", seed=16)
+    pr.check(pr.run(sd.Window(), False), 0, 2**31 - 1)
+    pr.check(pr.run(sd.Window(20, 2050), False), 20, 2050)
+
+
 def test_softmax_scale_and_large_scores(sd):
     for scale in (1.0, 0.01, 3.0):
         pr = Problem(sd, [129, 700], 8, 2, "paged", "f32", seed=5)
