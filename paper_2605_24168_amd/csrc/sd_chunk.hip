@@ -581,7 +581,10 @@ static int64_t chunk_tiles(const WindowParams &p, int rows) {
 void chunk_split(WindowParams &p, int kind) {
   const bool f32 = kind == kCacheF32;
   const int64_t keys = f32 ? kF32Keys * kWaves : kChunkKeys;
-  const int64_t blocks = chunk_tiles(p, f32 ? kF32Rows : kChunkRows) * p.hkv;
+  // (about as many row tiles: where sequences have less than one each, one)
+  const int64_t seqs = std::min<int64_t>(p.batch, p.n_rows);
+  const int64_t blocks =
+      std::max(p.n_rows * p.G / (f32 ? kF32Rows : kChunkRows) + seqs / 2, seqs) * p.hkv;
   int64_t seen = std::min<int64_t>(p.ncap, (int64_t)p.n_sink + p.window);
   const int64_t most = seen / (4 * keys);
   int64_t split = blocks > 0 ? 512 / blocks : 1;
