@@ -337,6 +337,16 @@ sd_status sparse_decode_set_debug(int32_t flags);
 sd_status sparse_decode_read_probe(const void *buf, size_t bytes, uint32_t *sink, void *stream);
 
 /* ------------------------------------------------------------------------
+ * The entry points from here to sparse_decode_pages_compact use no workspace:
+ * what they need between workgroups is in the static device array of
+ * sparse_decode_attention_noalloc.  They neither allocate nor free device
+ * memory and may be captured into graphs; as with every call here, calls and
+ * replays on one GPU must be ordered on one stream (or by events).
+ * Data pointers of queries, caches and outputs are 16-byte aligned
+ * (SD_ERR_INVALID_ARG otherwise).
+ */
+
+/* ------------------------------------------------------------------------
  * Attention with a sliding window and first tokens that stay visible.
  *
  * A query at position p sees the positions j <= p with j < n_sink or
@@ -368,15 +378,11 @@ typedef struct {
  * Positions that no query of the call sees are not read into any result,
  * whatever they hold.  Positions on pages outside the pool (a block table
  * entry below 0 or past its last page) are seen by no query.
- * Uses sparse_decode_window_workspace_size bytes of the library workspace.
  */
 sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,
                                          const int32_t *seq_lens, const int32_t *q_starts,
                                          int64_t batch, const sd_window *window, sd_tensor *out,
                                          void *stream);
-sd_status sparse_decode_window_workspace_size(const sd_tensor *q, const sd_kv *K, int64_t batch,
-                                              int32_t packed, const sd_window *window,
-                                              size_t *bytes);
 
 /* ------------------------------------------------------------------------
  * A key or value cache held in 4 bits.
@@ -433,13 +439,10 @@ sd_status sparse_decode_q4_load(const sd_kv4 *K, const sd_kv4 *V, const int32_t 
  *   q      [B, Hq, 128] bfloat16 (float32 returns SD_ERR_UNSUPPORTED)
  *   window NULL: every position of the sequence, scale 1/sqrt(128)
  *   out    [B, Hq, 128] bfloat16
- * Uses sparse_decode_q4_workspace_size bytes of the library workspace.
  */
 sd_status sparse_decode_q4_attention(const sd_tensor *q, const sd_kv4 *K, const sd_kv4 *V,
                                      const int32_t *seq_lens, const sd_window *window,
                                      sd_tensor *out, void *stream);
-sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K,
-                                          const sd_window *window, size_t *bytes);
 
 /* ------------------------------------------------------------------------
  * The pages of a paged cache.
@@ -451,7 +454,7 @@ sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K,
  * arrays are device memory that the calls below read and change; a pool is
  * any tensor whose first dimension counts pages (keys, values, labels, 4-bit
  * codes and scales).  Results do not depend on the order in which workgroups
- * run.  Entries outside [0, n_pages) and lengths outside [0, 16 max_pages]
+ * run.  Pools hold at most 2^23 pages.  Entries outside [0, n_pages) and lengths outside [0, 16 max_pages]
  * (read as clamped to it) are memory-safe.  Calls that change the same arrays
  * must be ordered on one stream. */
 typedef struct {
@@ -515,10 +518,6 @@ sd_status sparse_decode_pages_copy(const sd_tensor *pools, int32_t n_pools, cons
 sd_status sparse_decode_pages_compact(const sd_pages *pages, const sd_tensor *pools,
                                       int32_t n_pools, int32_t *remap, int32_t *n_live,
                                       void *stream);
-
-/* Bytes of the library workspace that the calls above need for this pool and
- * a table of at most `batch` rows. */
-sd_status sparse_decode_pages_workspace_size(int64_t n_pages, int64_t batch, size_t *bytes);
 
 const char *sparse_decode_status_string(sd_status status);
 

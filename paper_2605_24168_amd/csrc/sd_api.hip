@@ -1243,16 +1243,6 @@ sd::WindowParams window_params(const CacheShape &c, int64_t batch, int64_t rows,
   return p;
 }
 
-// Splits of a call (one query per sequence, or packed ones) and the bytes of
-// its partials.
-size_t window_work(sd::WindowParams &p, int kind, bool paged, bool packed) {
-  if (packed) sd::chunk_split(p, kind);
-  else sd::window_split(p, kind, paged);
-  if (p.nsplit <= 1) return 0;
-  return align_up((size_t)p.n_rows * p.hq * p.nsplit * sd::kPartStride * sizeof(float));
-}
-
-// The checks that window attention and its workspace size share.
 sd_status check_window_call(const sd_tensor *q, const sd_kv *K, int64_t batch, bool packed,
                             const sd_window *w, CacheShape &c, int64_t &rows, int64_t &hq) {
   if (!q || !K || !is_dtype_float(q->dtype)) return SD_ERR_INVALID_ARG;
@@ -1270,17 +1260,28 @@ sd_status check_window_call(const sd_tensor *q, const sd_kv *K, int64_t batch, b
   return SD_OK;
 }
 
+// The static scratch of the current device.  Every call of the entry points
+// below fits it by its limits on splits and pages, so they neither allocate
+// nor free, and a captured graph keeps a valid address.  Returns null with st
+// set on failure.  (Called with g_mu held.)
+char *static_scratch(size_t bytes, sd_status &st) {
+  DevState *ds = nullptr;
+  st = device_state(ds);
+  if (!st && bytes > kScratchBytes) st = SD_ERR_WORKSPACE;
+  return st ? nullptr : (char *)ds->scratch;
+}
+
 // Splits, scratch and launches of a call.
 sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
   const bool packed = p.q_starts != nullptr;
-  const size_t bytes = window_work(p, kind, paged, packed);
+  if (packed) sd::chunk_split(p, kind, kScratchBytes);
+  else sd::window_split(p, kind, paged);
   std::lock_guard<std::mutex> lk(g_mu);
-  if (bytes) {
-    DevState *ds = nullptr;
-    char *base = nullptr;
-    const sd_status st = get_workspace(bytes, ds, base);
+  if (p.nsplit > 1) {
+    sd_status st = SD_OK;
+    p.part = (float *)static_scratch(
+        (size_t)p.n_rows * p.hq * p.nsplit * sd::kPartStride * sizeof(float), st);
     if (st) return st;
-    p.part = (float *)base;
   }
   return hip_status(packed ? sd::launch_chunk_attend(p, kind, paged, (hipStream_t)stream)
                            : sd::launch_token_attend(p, kind, paged, (hipStream_t)stream));
@@ -1289,19 +1290,6 @@ sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
 }  // namespace
 
 extern "C" {
-
-sd_status sparse_decode_window_workspace_size(const sd_tensor *q, const sd_kv *K, int64_t batch,
-                                              int32_t packed, const sd_window *w, size_t *bytes) {
-  if (!bytes) return SD_ERR_INVALID_ARG;
-  CacheShape c;
-  int64_t rows = 0, hq = 0;
-  const sd_status st = check_window_call(q, K, batch, packed != 0, w, c, rows, hq);
-  if (st) return st;
-  sd::WindowParams p = window_params(c, batch, rows, hq, w);
-  *bytes = window_work(p, q->dtype == SD_F32 ? sd::kCacheF32 : sd::kCacheBf16, c.paged,
-                       packed != 0);
-  return SD_OK;
-}
 
 sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,
                                          const int32_t *seq_lens, const int32_t *q_starts,
@@ -1333,34 +1321,20 @@ sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, con
   return run_window(p, kind, c.paged, stream);
 }
 
-sd_status sparse_decode_q4_workspace_size(const sd_tensor *q, const sd_kv4 *K, const sd_window *w,
-                                          size_t *bytes) {
-  if (!bytes || !q) return SD_ERR_INVALID_ARG;
-  if (q->dtype == SD_F32) return SD_ERR_UNSUPPORTED;
-  CacheShape c;
-  int64_t rows = 0, hq = 0;
-  sd_status st = check_rows(q, SD_BF16, rows, hq);
-  if (!st) st = check_batch(rows);
-  if (!st && w) st = check_window(w);
-  if (!st) st = check_kv4(K, rows, c);
-  if (st) return st;
-  if (hq % c.hkv) return SD_ERR_INVALID_ARG;
-  if (hq / c.hkv > sd::kMaxGroup) return SD_ERR_UNSUPPORTED;
-  sd::WindowParams p = window_params(c, rows, rows, hq, w);
-  *bytes = window_work(p, sd::kCacheQ4, c.paged, false);
-  return SD_OK;
-}
-
 sd_status sparse_decode_q4_attention(const sd_tensor *q, const sd_kv4 *K, const sd_kv4 *V,
                                      const int32_t *seq_lens, const sd_window *w, sd_tensor *out,
                                      void *stream) {
-  size_t unused = 0;
-  sd_status st = sparse_decode_q4_workspace_size(q, K, w, &unused);
-  if (st) return st;
-  const int64_t batch = q->shape[0], hq = q->shape[1];
+  if (!q) return SD_ERR_INVALID_ARG;
+  if (q->dtype == SD_F32) return SD_ERR_UNSUPPORTED;
+  int64_t batch = 0, hq = 0;
+  sd_status st = check_rows(q, SD_BF16, batch, hq);
+  if (!st) st = check_batch(batch);
+  if (!st && w) st = check_window(w);
   CacheShape c;
-  st = check_pair4(K, V, batch, c);
+  if (!st) st = check_pair4(K, V, batch, c);
   if (st) return st;
+  if (hq % c.hkv) return SD_ERR_INVALID_ARG;
+  if (hq / c.hkv > sd::kMaxGroup) return SD_ERR_UNSUPPORTED;
   int64_t rows = 0, heads = 0;
   st = check_rows(out, SD_BF16, rows, heads);
   if (st) return st;
@@ -1441,7 +1415,7 @@ sd_status sparse_decode_q4_load(const sd_kv4 *K, const sd_kv4 *V, const int32_t 
 
 namespace {
 
-constexpr int64_t kMaxPages = int64_t(1) << 28;
+constexpr int64_t kMaxPages = int64_t(1) << 23;
 
 sd_status check_pages(const sd_pages *p) {
   if (!p || p->n_pages < 0 || p->batch < 0 || p->max_pages < 0) return SD_ERR_INVALID_ARG;
@@ -1497,26 +1471,18 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   return na && nb && x < y + nb && y < x + na;
 }
 
-// The workspace of the page calls, as f(base).
+// The scratch of the page calls, as f(base).
 template <class F>
 sd_status with_pages_work(int64_t n_pages, int64_t batch, F f) {
   std::lock_guard<std::mutex> lk(g_mu);
-  DevState *ds = nullptr;
-  char *base = nullptr;
-  const sd_status st = get_workspace(sd::pages_work_bytes(n_pages, batch), ds, base);
+  sd_status st = SD_OK;
+  char *base = static_scratch(sd::pages_work_bytes(n_pages, batch), st);
   return st ? st : hip_status(f(base));
 }
 
 }  // namespace
 
 extern "C" {
-
-sd_status sparse_decode_pages_workspace_size(int64_t n_pages, int64_t batch, size_t *bytes) {
-  if (!bytes || n_pages < 0 || batch < 0) return SD_ERR_INVALID_ARG;
-  if (n_pages > kMaxPages || batch > 65535) return SD_ERR_UNSUPPORTED;
-  *bytes = sd::pages_work_bytes(n_pages, batch);
-  return SD_OK;
-}
 
 sd_status sparse_decode_pages_extend(const sd_pages *pages, const int32_t *grow, int32_t *status,
                                      void *stream) {

@@ -43,8 +43,9 @@ struct WindowParams {
 // Splits of one sequence and KV head over workgroups, from what the host
 // knows (see window_split); fills p.span, p.nsplit and p.quad.
 void window_split(WindowParams &p, int kind, bool paged);
-// The same for packed queries; fills p.nsplit.
-void chunk_split(WindowParams &p, int kind);
+// The same for packed queries, with partials of at most `scratch` bytes; fills
+// p.nsplit.
+void chunk_split(WindowParams &p, int kind, size_t scratch);
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 

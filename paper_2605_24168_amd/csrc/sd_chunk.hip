@@ -578,7 +578,7 @@ static int64_t chunk_tiles(const WindowParams &p, int rows) {
 // Calls with few rows split what they see over workgroups, so that about two
 // workgroups run on each of the 256 compute units, at least four tiles for
 // each.
-void chunk_split(WindowParams &p, int kind) {
+void chunk_split(WindowParams &p, int kind, size_t scratch) {
   const bool f32 = kind == kCacheF32;
   const int64_t keys = f32 ? kF32Keys * kWaves : kChunkKeys;
   // (about as many row tiles: where sequences have less than one each, one)
@@ -589,6 +589,8 @@ void chunk_split(WindowParams &p, int kind) {
   const int64_t most = seen / (4 * keys);
   int64_t split = blocks > 0 ? 512 / blocks : 1;
   split = std::min<int64_t>(split, most);
+  const int64_t row = (int64_t)(kPartStride * sizeof(float)) * p.hq * p.n_rows;
+  split = std::min<int64_t>(split, row > 0 ? (int64_t)scratch / row : 1);
   p.nsplit = (int32_t)std::max<int64_t>(split, 1);
 }
 

@@ -29,8 +29,8 @@ struct PageWork {
   int32_t *first;     // [batch]: extend: rank of the row's first page
   int32_t *have;      // [batch]: extend: pages it held; fork: children of a parent
   int32_t *eldest;    // [batch]: fork: a parent's first child
-  int32_t *list;      // [pages]: compact: movers; fork: a child's own last page
-  int32_t *hole;      // [pages]: compact: holes; fork: [0, batch) a child's rank among those
+  int32_t *list;      // [pages / 2]: compact: movers; fork: a child's own last page
+  int32_t *hole;      // [pages / 2]: compact: holes; fork: [0, batch) a child's rank among those
                       // that get a page, [batch, ..) the page that it copies
 };
 enum { kLimit = 0, kMoves = 1, kLive = 2 };
@@ -52,8 +52,8 @@ static size_t carve_pages(int64_t n_pages, int64_t batch, char *base, PageWork *
   x.first = take(batch);
   x.have = take(batch);
   x.eldest = take(batch);
-  x.list = take(n_pages > batch ? n_pages : batch);
-  x.hole = take(n_pages > 2 * batch ? n_pages : 2 * batch);
+  x.list = take(std::max(n_pages / 2, batch));
+  x.hole = take(std::max(n_pages / 2, 2 * batch));
   if (w) *w = x;
   return at;
 }

@@ -147,23 +147,19 @@ lib.sparse_decode_sampled_attention.argtypes = [_P(SdTensor), _P(SdKv), _P(SdKv)
 for _name, _args in {
         "window_attention": [_P(SdTensor), _P(SdKv), _P(SdKv), C.c_void_p, C.c_void_p, C.c_int64,
                              _P(SdWindow), _P(SdTensor), C.c_void_p],
-        "window_workspace_size": [_P(SdTensor), _P(SdKv), C.c_int64, C.c_int32, _P(SdWindow),
-                                  _P(C.c_size_t)],
         "q4_append": [_P(SdTensor), _P(SdTensor), _P(SdKv4), _P(SdKv4), C.c_void_p, C.c_void_p,
                       C.c_int64, C.c_void_p],
         "q4_load": [_P(SdKv4), _P(SdKv4), C.c_void_p, C.c_void_p, C.c_int64, _P(SdTensor),
                     _P(SdTensor), C.c_void_p],
         "q4_attention": [_P(SdTensor), _P(SdKv4), _P(SdKv4), C.c_void_p, _P(SdWindow),
                          _P(SdTensor), C.c_void_p],
-        "q4_workspace_size": [_P(SdTensor), _P(SdKv4), _P(SdWindow), _P(C.c_size_t)],
         "pages_extend": [_P(SdPages), C.c_void_p, C.c_void_p, C.c_void_p],
         "pages_fork": [_P(SdPages), _P(SdPages), C.c_void_p, C.c_int32, _P(SdTensor), C.c_int32,
                        C.c_void_p, C.c_void_p],
         "pages_free": [_P(SdPages), C.c_void_p, C.c_int64, C.c_void_p],
         "pages_copy": [_P(SdTensor), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p],
         "pages_compact": [_P(SdPages), _P(SdTensor), C.c_int32, C.c_void_p, C.c_void_p,
-                          C.c_void_p],
-        "pages_workspace_size": [C.c_int64, C.c_int64, _P(C.c_size_t)]}.items():
+                          C.c_void_p]}.items():
     getattr(lib, f"sparse_decode_{_name}").restype = C.c_int
     getattr(lib, f"sparse_decode_{_name}").argtypes = _args
 lib.sparse_decode_read_probe.restype = C.c_int
@@ -177,9 +173,8 @@ _raw = C.CDLL(LIB_PATH)
 for _name in ("score", "topk", "attend", "attend_weighted", "dense_attention",
               "dense_workspace_size", "label_attention", "label_score", "attention",
               "attention_noalloc", "workspace_size", "budget", "sampled_attention",
-              "window_attention", "window_workspace_size", "q4_append", "q4_load", "q4_attention",
-              "q4_workspace_size", "pages_extend", "pages_fork", "pages_free", "pages_copy",
-              "pages_compact"):
+              "window_attention", "q4_append", "q4_load", "q4_attention", "pages_extend",
+              "pages_fork", "pages_free", "pages_copy", "pages_compact"):
     _f, _g = getattr(lib, f"sparse_decode_{_name}"), getattr(_raw, f"sparse_decode_{_name}")
     _g.restype = _f.restype
     _g.argtypes = [C.c_void_p if _t in (_P(SdTensor), _P(SdKv), _P(SdSparsity), _P(SdLabels),
@@ -789,16 +784,6 @@ def sparse_decode_window_attention(q, cache: KVCache, seq_lens, window: Window, 
     return out
 
 
-def window_workspace_size(q, cache: KVCache, seq_lens, window: Window, q_starts=None) -> int:
-    n = C.c_size_t(0)
-    batch = _batch_of(cache, seq_lens, q_starts)
-    cq, kk, cw = _desc(q, "q"), _kv_desc(cache, "k"), _window_desc(window)
-    _check(_raw.sparse_decode_window_workspace_size(cq, kk, batch, int(q_starts is not None), cw,
-                                                    C.byref(n)),
-           "sparse_decode_window_workspace_size")
-    return int(n.value)
-
-
 def sparse_decode_q4_append(k, v, cache: Q4Cache, seq_lens, starts=None, stream=None) -> None:
     """Write the rows of k and v [T, Hkv, 128] as the last positions of their
     sequences (seq_lens counts them): row b of sequence b, or with starts
@@ -846,15 +831,6 @@ def sparse_decode_q4_attention(q, cache: Q4Cache, seq_lens, window: Optional[Win
     cw = _window_desc(window) if window is not None else None
     _call(_raw.sparse_decode_q4_attention, q.get_device(), stream, cq, kk, kv, seq_lens.data_ptr(), cw, co)
     return out
-
-
-def q4_workspace_size(q, cache: Q4Cache, window: Optional[Window] = None) -> int:
-    n = C.c_size_t(0)
-    cq, (kk, _) = _desc(q, "q"), _q4_descs(cache)
-    cw = _window_desc(window) if window is not None else None
-    _check(_raw.sparse_decode_q4_workspace_size(cq, kk, cw, C.byref(n)),
-           "sparse_decode_q4_workspace_size")
-    return int(n.value)
 
 
 def _pages_desc(pages: Pages) -> bytes:
@@ -942,13 +918,6 @@ def sparse_decode_pages_compact(pages: Pages, pools: Sequence[torch.Tensor] = ()
     _call(_raw.sparse_decode_pages_compact, dev.index, stream, cp, pl, count, remap.data_ptr(),
           n_live.data_ptr())
     return remap, n_live
-
-
-def pages_workspace_size(n_pages: int, batch: int) -> int:
-    n = C.c_size_t(0)
-    _check(lib.sparse_decode_pages_workspace_size(int(n_pages), int(batch), C.byref(n)),
-           "sparse_decode_pages_workspace_size")
-    return int(n.value)
 
 
 def read_probe(buf: torch.Tensor, sink: torch.Tensor, stream=None) -> None:

@@ -209,23 +209,18 @@ def test_captured_beam_steps(sd):
             m.table, m.lens = table, lens
             if step == 0:
                 m.extend(g)
-    need = sd.pages_workspace_size(pages, rows)
-    try:
-        sd.set_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"))
+    pair()
+    model_pair([0] * rows, [0] * rows)
+    same(m, a, pools)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
         pair()
-        model_pair([0] * rows, [0] * rows)
+    for step in range(5):
+        parents, g = rng.integers(0, rows, rows), rng.integers(0, 9, rows)
+        par.copy_(cuda(parents))
+        grow.copy_(cuda(g))
+        graph.replay()
+        torch.cuda.synchronize()
+        model_pair(parents, g)
         same(m, a, pools)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            pair()
-        for step in range(5):
-            parents, g = rng.integers(0, rows, rows), rng.integers(0, 9, rows)
-            par.copy_(cuda(parents))
-            grow.copy_(cuda(g))
-            graph.replay()
-            torch.cuda.synchronize()
-            model_pair(parents, g)
-            same(m, a, pools)
-            assert (b.block_table == -1).all() and (b.seq_lens == 0).all()
-    finally:
-        sd.set_workspace(None)
+        assert (b.block_table == -1).all() and (b.seq_lens == 0).all()

@@ -246,22 +246,17 @@ def test_replayed_graphs_and_other_streams(sd):
             (out * 2).sum().item()
 
 
-def test_workspace_size_is_enough_and_checked(sd):
-    pr = Problem(sd, [20000], 4, 1, "bhnd", "bf16", seed=13)
-    q = pr.q.cuda()
-    need = sd.window_workspace_size(q, pr.cache, pr.dev_lens, sd.Window())
-    assert need > 0
-    eager = pr.run(sd.Window(), False)
-    try:
-        buf = torch.empty(need, dtype=torch.uint8, device="cuda")
-        sd.set_workspace(buf)
-        assert torch.equal(pr.run(sd.Window(), False), eager)
-        sd.set_workspace(buf[:need - 256])
-        with pytest.raises(sd.SparseDecodeError) as e:
-            pr.run(sd.Window(), False)
-        assert e.value.status == sd.SD_ERR_WORKSPACE
-    finally:
-        sd.set_workspace(None)
+def test_no_workspace_is_used(sd):
+    # Split calls with a caller's workspace too small for any partial.
+    for counts in (None, [3]):
+        pr = Problem(sd, [20000], 4, 1, "bhnd", "bf16", counts=counts, seed=13)
+        eager = pr.run(sd.Window(), counts is not None)
+        try:
+            sd.set_workspace(torch.empty(256, dtype=torch.uint8, device="cuda"))
+            assert torch.equal(pr.run(sd.Window(), counts is not None), eager)
+        finally:
+            sd.set_workspace(None)
+        pr.check(eager, 0, 2**31 - 1)
 
 
 def test_offsets_past_32_bits(sd):
