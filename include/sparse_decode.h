@@ -376,7 +376,8 @@ typedef struct {
  *   batch    sequences: the rows of seq_lens (and of the block table)
  *   out      [T, Hq, 128], dtype of q; may not overlap an input
  * Positions that no query of the call sees are not read into any result,
- * whatever they hold.  Positions on pages outside the pool (a block table
+ * whatever they hold.  (NaN or infinity where one query of a sequence sees it
+ * is undefined for that sequence's other queries of the call too.)  Positions on pages outside the pool (a block table
  * entry below 0 or past its last page) are seen by no query.
  */
 sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,

@@ -96,6 +96,7 @@ struct ChunkRange {
     pmax = position(p, it, it.row0 + ROWS - 1);
     sink = min(p.n_sink, pmax + 1);
     lo = pmin + 1 > p.window ? pmin + 1 - p.window : 0;
+    if (p.window == 0) lo = max(pmax + 1, 0);   // no window at all
     na = sink > 0 ? (sink + KEYS - 1) / KEYS : 0;
     b0 = lo / KEYS;
     b0 = b0 < na ? na : b0;
@@ -434,7 +435,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
     const int j0 = cr.first_of(t);
     const uint32_t gone = PAGED ? (uint32_t)(outside >> (4 * (t - held))) & 15u : 0u;
     const bool whole = !gone && j0 + kChunkKeys <= wmin + 1 &&
-                       (j0 + kChunkKeys <= p.n_sink || j0 > wmax - p.window);
+                       (j0 + kChunkKeys <= p.n_sink || wmax - j0 < p.window);
     if (!whole) {
 #pragma unroll
       for (int y = 0; y < 2; ++y)

@@ -220,6 +220,16 @@ def test_positions_between_sinks_and_window_may_hold_anything(sd):
                 pr.check(pr.run(sd.Window(10, 100), counts is not None), 10, 100)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_without_a_window_only_the_first_tokens_are_read(sd, dtype):
+    for counts in (None, [40], [300]):
+        pr = Problem(sd, [300], 4, 2, "bhnd", dtype, counts=counts, seed=17)
+        for bad in (float("nan"), float("inf")):
+            pr.cache.k[0, :, 5:300] = bad
+            pr.cache.v[0, :, 5:300] = bad
+            pr.check(pr.run(sd.Window(5, 0), counts is not None), 5, 0)
+
+
 def test_replayed_graphs_and_other_streams(sd):
     for counts in (None, [33, 1]):
         pr = Problem(sd, [3000, 600], 8, 2, "paged", "bf16", counts=counts, seed=12)
