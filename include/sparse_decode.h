@@ -376,9 +376,11 @@ typedef struct {
  *   batch    sequences: the rows of seq_lens (and of the block table)
  *   out      [T, Hq, 128], dtype of q; may not overlap an input
  * Positions that no query of the call sees are not read into any result,
- * whatever they hold.  (NaN or infinity where one query of a sequence sees it
- * is undefined for that sequence's other queries of the call too.)  Positions on pages outside the pool (a block table
- * entry below 0 or past its last page) are seen by no query.
+ * whatever they hold.  NaN where a query sees it reaches its output; NaN or
+ * infinity that one query of a sequence sees leaves that sequence's other
+ * queries of the call undefined.  Positions on pages outside the pool (a block
+ * table entry below 0 or past its last page) are seen by no query.  Scores are
+ * at most 2^28 in magnitude (rounding them to 32 bits would move weights).
  */
 sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,
                                          const int32_t *seq_lens, const int32_t *q_starts,
@@ -455,9 +457,9 @@ sd_status sparse_decode_q4_attention(const sd_tensor *q, const sd_kv4 *K, const 
  * arrays are device memory that the calls below read and change; a pool is
  * any tensor whose first dimension counts pages (keys, values, labels, 4-bit
  * codes and scales).  Results do not depend on the order in which workgroups
- * run.  Pools hold at most 2^23 pages.  Entries outside [0, n_pages) and lengths outside [0, 16 max_pages]
- * (read as clamped to it) are memory-safe.  Calls that change the same arrays
- * must be ordered on one stream. */
+ * run.  Pools hold at most 2^23 pages.  Entries outside [0, n_pages) and
+ * lengths outside [0, 16 max_pages] (read as clamped to it) are memory-safe.
+ * Calls that change the same arrays must be ordered on one stream. */
 typedef struct {
   int32_t *block_table;  /* device int32 [batch, max_pages] */
   int32_t *seq_lens;     /* device int32 [batch]            */

@@ -144,7 +144,7 @@ __device__ __forceinline__ Joined join_splits(const float *pp, int n) {
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (NaN stays NaN)
   return Joined{x * inv, y * inv};
 }
 

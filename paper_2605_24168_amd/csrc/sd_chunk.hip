@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
     pp[0] = M;
     pp[1] = sum;
   }
-  const float inv = p.nsplit > 1 ? 1.f : (sum > 0.f ? 1.f / sum : 0.f);
+  const float inv = p.nsplit > 1 ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
   for (int i = threadIdx.x >> 5; i < 32; i += kBlock / 32) {
     const int c = 4 * i, at = col * (kHeadDim + 4) + c;
     const f32x4 x = (*(f32x4 *)&lds_o[0][at] + *(f32x4 *)&lds_o[1][at]) * inv;
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
       for (int r = 0; r < 16; ++r) pp[2 + 32 * c + 8 * (r >> 2) + 4 * half + (r & 3)] = acc[c][r];
     return;
   }
-  const float inv = ls > 0.f ? 1.f / ls : 0.f;
+  const float inv = ls == 0.f ? 0.f : 1.f / ls;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll

@@ -461,7 +461,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
       v += f * o[row * kRow + c];
     }
     if (nsp == 1) {
-      store_out<KIND>(p, (orow + hh) * kHeadDim + c, sum > 0.f ? v / sum : 0.f);
+      store_out<KIND>(p, (orow + hh) * kHeadDim + c, sum == 0.f ? 0.f : v / sum);
     } else {
       float *pp = p.part + ((orow + hh) * p.nsplit + s) * kPartStride;
       if (c == 0) {

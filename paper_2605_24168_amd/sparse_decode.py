@@ -779,8 +779,9 @@ def sparse_decode_window_attention(q, cache: KVCache, seq_lens, window: Window, 
         out = _empty_like(q, stream)
     _same_device(q, cache.k, cache.v, cache.block_table, seq_lens, q_starts, out)
     cq, (kk, kv), co = _desc(q, "q"), _kv_desc(cache, "k", "v"), _desc(out, "out")
-    _call(_raw.sparse_decode_window_attention, q.get_device(), stream, cq, kk, kv, seq_lens.data_ptr(),
-          q_starts.data_ptr() if q_starts is not None else None, batch, _window_desc(window), co)
+    _call(_raw.sparse_decode_window_attention, q.get_device(), stream, cq, kk, kv,
+          seq_lens.data_ptr(), q_starts.data_ptr() if q_starts is not None else None, batch,
+          _window_desc(window), co)
     return out
 
 
@@ -829,7 +830,8 @@ def sparse_decode_q4_attention(q, cache: Q4Cache, seq_lens, window: Optional[Win
     _same_device(q, *cache.pools, cache.block_table, seq_lens, out)
     cq, (kk, kv), co = _desc(q, "q"), _q4_descs(cache), _desc(out, "out")
     cw = _window_desc(window) if window is not None else None
-    _call(_raw.sparse_decode_q4_attention, q.get_device(), stream, cq, kk, kv, seq_lens.data_ptr(), cw, co)
+    _call(_raw.sparse_decode_q4_attention, q.get_device(), stream, cq, kk, kv,
+          seq_lens.data_ptr(), cw, co)
     return out
 
 
@@ -861,7 +863,8 @@ def sparse_decode_pages_extend(pages: Pages, grow, status=None, stream=None):
     status = _empty((batch,), torch.int32, dev, stream) if status is None else status
     _need_vector(status, "status", batch)
     _same_device(pages.block_table, grow, status)
-    _call(_raw.sparse_decode_pages_extend, dev.index, stream, cp, grow.data_ptr(), status.data_ptr())
+    _call(_raw.sparse_decode_pages_extend, dev.index, stream, cp, grow.data_ptr(),
+          status.data_ptr())
     return status
 
 
@@ -878,8 +881,8 @@ def sparse_decode_pages_fork(pages: Pages, to: Pages, parents, pools: Sequence[t
     _need_vector(status, "status", batch)
     _same_device(pages.block_table, to.block_table, parents, status)
     pl, n = _pools_desc(pools, dev)
-    _call(_raw.sparse_decode_pages_fork, dev.index, stream, cp, ct, parents.data_ptr(), int(bool(keep)), pl,
-          n, status.data_ptr())
+    _call(_raw.sparse_decode_pages_fork, dev.index, stream, cp, ct, parents.data_ptr(),
+          int(bool(keep)), pl, n, status.data_ptr())
     return status
 
 
@@ -888,7 +891,8 @@ def sparse_decode_pages_free(pages: Pages, rows, stream=None) -> None:
     cp = _pages_desc(pages)
     _need_vector(rows, "rows")
     _same_device(pages.block_table, rows)
-    _call(_raw.sparse_decode_pages_free, rows.get_device(), stream, cp, rows.data_ptr(), rows.shape[0])
+    _call(_raw.sparse_decode_pages_free, rows.get_device(), stream, cp, rows.data_ptr(),
+          rows.shape[0])
 
 
 def sparse_decode_pages_copy(pools: Sequence[torch.Tensor], src, dst, stream=None) -> None:
@@ -898,8 +902,8 @@ def sparse_decode_pages_copy(pools: Sequence[torch.Tensor], src, dst, stream=Non
     _need_vector(dst, "dst", int(src.shape[0]))
     _same_device(src, dst)
     pl, n = _pools_desc(pools, src.device)
-    _call(_raw.sparse_decode_pages_copy, src.get_device(), stream, pl, n, src.data_ptr(), dst.data_ptr(),
-          src.shape[0])
+    _call(_raw.sparse_decode_pages_copy, src.get_device(), stream, pl, n, src.data_ptr(),
+          dst.data_ptr(), src.shape[0])
 
 
 def sparse_decode_pages_compact(pages: Pages, pools: Sequence[torch.Tensor] = (), remap=None,

@@ -237,6 +237,20 @@ def test_attention_skips_pages_outside_the_pool(sd):
     check_attention(sd, [40, 400], 4, 2, "paged", 32, 350, seed=6, hide=hide, change=change)
 
 
+@pytest.mark.parametrize("layout", ["bhnd", "paged"])
+def test_groups_that_are_not_numbers_reach_the_output(sd, layout):
+    lens = [3000, 40]
+    c, _ = random_cache(sd, lens, 2, layout, seed=8)
+    q = torch.randn((2, 4, 128), device="cuda").bfloat16()
+    dl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    at = (0, 0, 2990) if layout == "bhnd" else (int(c.block_table[0, 2990 // 16]), 0, 2990 % 16)
+    for scales, channels in ((c.v_scales, range(32, 64)), (c.k_scales, range(128))):
+        scales[(*at, 1)] = 255
+        nan = torch.isnan(sd.sparse_decode_q4_attention(q, c, dl)).cpu()
+        assert nan[0, :2, list(channels)].all()
+        assert nan.sum() == 2 * len(channels)
+
+
 def test_replayed_step(sd):
     """Append, then attend, captured once and replayed with new tokens."""
     B, hq, hkv, cap = 3, 8, 2, 500

@@ -230,6 +230,24 @@ def test_without_a_window_only_the_first_tokens_are_read(sd, dtype):
             pr.check(pr.run(sd.Window(5, 0), counts is not None), 5, 0)
 
 
+@pytest.mark.parametrize("layout", ["bhnd", "paged"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts", [None, [33, 1], [2, 7]])
+def test_a_nan_that_a_query_sees_reaches_its_output(sd, dtype, layout, counts):
+    # Sequence 0's last query sees the position; sequence 1 and the other KV
+    # head do not.  (3000 positions: over several workgroups.)
+    pr = Problem(sd, [3000, 40], 4, 2, layout, dtype, counts=counts, seed=18)
+    at = (0, 0, 2990) if layout == "bhnd" else (int(pr.table[0, 2990 // 16]), 2990 % 16, 0)
+    last, w = (0 if counts is None else counts[0] - 1), sd.Window(0, 2500)
+    for t, channels in ((pr.cache.v, [5]), (pr.cache.k, list(range(128)))):
+        t[(*at, 5)] = float("nan")
+        out = pr.run(w, counts is not None)
+        nan = torch.isnan(out).cpu()
+        assert nan[last, :2, channels].all()
+        assert nan[last, :2].sum() == 2 * len(channels)
+        assert not nan[:, 2:].any() and not nan[last + 1:].any()
+
+
 def test_replayed_graphs_and_other_streams(sd):
     for counts in (None, [33, 1]):
         pr = Problem(sd, [3000, 600], 8, 2, "paged", "bf16", counts=counts, seed=12)
