@@ -3,11 +3,11 @@
 // tokens leave visible, on float32 and bfloat16 caches.
 //
 // Bound by the matrix unit: 4 * 128 operations per query head and visible
-// position.  A workgroup takes 128 rows of one KV head, a row being one query
-// head of one token (the G heads of a token follow each other), so that
-// grouped heads share every key and value tile, and short chunks still fill
-// the tiles.  Each of its four waves owns 32 rows and walks all tiles of 64
-// positions, which the workgroup stages in LDS.
+// position.  A workgroup takes rows of one KV head, a row being one query head
+// of one token (the G heads of a token follow each other), so that grouped
+// heads share every key and value tile, and short chunks still fill the tiles.
+// In bfloat16 it takes 128: each of its four waves owns 32 and walks all tiles
+// of 64 positions, which the workgroup stages in LDS.
 //
 // S = K q^T by 32x32 matrix instructions with the keys as the first operand
 // leaves lane (row = lane & 31, half = lane >> 5) the scores of positions
@@ -15,7 +15,7 @@
 // exchange between two lanes, and the weights are the second operand of
 // O^T = V^T p^T as they lie in the registers: the contraction takes the
 // positions in that order, and V's operand is read in the same one, by
-// transposing LDS reads (bfloat16) or plain ones (float32).
+// transposing LDS reads (bfloat16) or rows from memory (float32).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,6 +26,7 @@
 namespace sd {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunkRows = 128;      // rows of a workgroup
@@ -138,13 +139,15 @@ __device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, int &
 }
 
 // ---------------------------------------------------------------------------
-// float32: bound by the matrix unit at a sixteenth of its bfloat16 rate, so
+// float32: bound by the matrix unit, at an eighth of its bfloat16 rate, so
 // operands come straight from global memory.  The four waves of a workgroup
 // share 32 rows and take every fourth tile of 32 positions each; they join at
-// the end.  Keys and values use the same registers, one after the other, so
-// that two waves fit a SIMD and wait for their loads in turn (both in registers
-// and one wave per SIMD: 77 instead of 62 us for 1.3K tokens of 8 heads over a
-// window of 511, 611 instead of 556 us for 1024 tokens of 32 heads over 4096).
+// the end.  Keys and values pass through the same registers: each group of
+// four matrix instructions is followed by the load that refills its operand,
+// values behind keys and the next tile's keys behind values, so that sixteen
+// loads are always under way and each has half a tile's time to arrive.
+// 1024 tokens of 32 heads over 4096 positions: 470 us, 128 TFLOP/s of the 153
+// that a large product reaches (loads left to the compiler, two under way: 561).
 // ---------------------------------------------------------------------------
 constexpr int kF32Rows = 32;
 constexpr int kF32Keys = 32;
@@ -190,6 +193,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
         continue;
       }
       int page = j <= cr.pmax ? p.block_table[(int64_t)it.b * p.max_pages + (j >> 4)] : 0;
+      page = __builtin_amdgcn_readfirstlane(page);
       if (page < 0 || page >= p.n_pages) {
         page = 0;
         x.bad |= 0xFFFFu << (16 * i);
@@ -198,45 +202,69 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
     }
     return x;
   };
-  // Row x of the tile at j0, in bytes.  (A page has all its rows; of a
-  // contiguous cache, only those up to the last position may be read.)
-  auto row_at = [&](const Where &wh, int j0, int x) {
-    const int y = PAGED ? x : min(x, cr.pmax - j0);
-    return PAGED ? (x < kTile ? wh.at[0] : wh.at[1]) + (int64_t)((y & 15) * step)
-                 : wh.at[0] + (int64_t)(y * step);
+  // Sixteen loads bring a wave's tile of keys, piece i (channels 8 i + 4 half ..)
+  // of row col each, and sixteen its values, row 8 (i / 4) + 4 half + i % 4 at
+  // channels 4 col ..  (A page has all its rows; of a contiguous cache, only
+  // those up to the last position may be read.)
+  auto key_row = [&](const Where &wh, int j0) {
+    const int y = PAGED ? col & 15 : min(col, cr.pmax - j0);
+    return p.k + (PAGED && col >= kTile ? wh.at[1] : wh.at[0]) + (int64_t)(y * step) + 16 * half;
   };
-  for (int t = cr.t0 + w; t < cr.t1; t += kWaves) {
-    const int j0 = cr.first_of(t);
-    const Where now = locate(j0);
-    f32x4 kf[16], vf[16];
-    const char *src = p.k + row_at(now, j0, col) + 16 * half;
+  auto value = [&](const Where &wh, int j0, int i) {
+    int y = 8 * (i >> 2) + (i & 3), z = 4 * half;
+    if (PAGED) {
+      y &= 15;
+    } else {
+      const int last = cr.pmax - j0;
+      y = min(y, last);
+      z = min(z, last - y);
+    }
+    return *(const f32x4 *)(p.v + wh.at[PAGED ? i >> 3 : 0] + (int64_t)y * step +
+                            (uint32_t)(z * step + 16 * col));
+  };
+  f32x4 x[16];   // keys, then the values, then the next tile's keys
+  Where next{};
+  if (cr.t0 + w < cr.t1) {
+    next = locate(cr.first_of(cr.t0 + w));
+    const char *src = key_row(next, cr.first_of(cr.t0 + w));
 #pragma unroll
-    for (int i = 0; i < 16; ++i) kf[i] = *(const f32x4 *)(src + 32 * i);
+    for (int i = 0; i < 16; ++i) x[i] = *(const f32x4 *)(src + 32 * i);
+  }
+  for (int t = cr.t0 + w; t < cr.t1; t += kWaves) {
+    const int j0 = cr.first_of(t), jn = cr.first_of(t + kWaves < cr.t1 ? t + kWaves : t);
+    const Where now = next;
+    next = locate(jn);
     f32x16 sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+    f32x4 qf = *(const f32x4 *)&lds_q[(half * 32 + col) * 4];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const f32x4 qf = *(const f32x4 *)&lds_q[((2 * i + half) * 32 + col) * 4];
+      const f32x4 q0 = qf;
+      if (i < 15) qf = *(const f32x4 *)&lds_q[((2 * i + 2 + half) * 32 + col) * 4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i][e], qf[e], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i][e], q0[e], sc, 0, 0, 0);
+      x[i] = value(now, j0, i);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);   // (the values take the keys' registers)
+    // Every row sees all of the tile, or some see part of it.
+    const bool whole = !now.bad && j0 + kF32Keys <= cr.pmin + 1 &&
+                       (j0 + kF32Keys <= p.n_sink || cr.pmax - j0 < p.window);
+    if (!whole) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      vf[r] = *(const f32x4 *)(p.v + row_at(now, j0, 8 * (r >> 2) + 4 * half + (r & 3)) + 16 * col);
-    float top = -__builtin_inff();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int x = 8 * (r >> 2) + 4 * half + (r & 3), j = j0 + x;
-      const bool sees = (j < row.first) | ((uint32_t)(row.pos - j) < (uint32_t)p.window);
-      const bool there = !(now.bad >> x & 1);
-      sc[r] = (sees & there) ? sc[r] : -__builtin_inff();
-      top = fmaxf(top, sc[r]);
-      // A position that no row sees weighs 0, whatever its values hold.
-      if (!there || j > cr.pmax || (j >= cr.sink && j < cr.lo)) vf[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < 16; ++r) {
+        const int y = 8 * (r >> 2) + 4 * half + (r & 3), j = j0 + y;
+        const bool sees = (j < row.first) | ((uint32_t)(row.pos - j) < (uint32_t)p.window);
+        const bool there = !(now.bad >> y & 1);
+        sc[r] = (sees & there) ? sc[r] : -__builtin_inff();
+        // A position that no row sees weighs 0, whatever its values hold.
+        if (!there || j > cr.pmax || (j >= cr.sink && j < cr.lo)) x[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     }
+    float top = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
     if (__ballot(top * p.scale2 > m + kChunkSlack)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float mn = fmaxf(m, top * p.scale2);
@@ -251,11 +279,16 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
       sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], p.scale2, -m));
       ls += sc[r];
     }
+    const char *src = key_row(next, jn);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int r = 0; r < 16; ++r) {
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][c], sc[r], acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[r][c], sc[r], acc[c], 0, 0, 0);
+      x[r] = *(const f32x4 *)(src + 32 * r);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   // Join the waves: to the common maximum, then pairwise sums of outputs.
@@ -286,22 +319,26 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
   __syncthreads();
   if (w < 2) each([&](int c, f32x4 x) { *(f32x4 *)(mine + c) = x + *(f32x4 *)(mine + c); });
   __syncthreads();
-  if (!row.live) return;
-  const int64_t orow = row.at / kHeadDim;
-  float *pp = p.part + (orow * p.nsplit + split) * kPartStride;
-  if (p.nsplit > 1 && threadIdx.x < 32) {
-    pp[0] = M;
-    pp[1] = sum;
-  }
+  // Whole rows, 32 lanes each.  (Lane `col` has that row's maximum and sum.)
   const float inv = p.nsplit > 1 ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
-  for (int i = threadIdx.x >> 5; i < 32; i += kBlock / 32) {
-    const int c = 4 * i, at = col * (kHeadDim + 4) + c;
-    const f32x4 x = (*(f32x4 *)&lds_o[0][at] + *(f32x4 *)&lds_o[1][at]) * inv;
-    if (p.nsplit == 1) {
-      *(f32x4 *)((float *)p.out + row.at + c) = x;
-    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pp[2 + c + e] = x[e];
+  for (int i = 0; i < 4; ++i) {
+    const int r = 2 * w + 8 * i + half;   // lanes r and r + 32 hold row r
+    const float scale = __shfl(inv, r), rm = __shfl(M, r), rs = __shfl(sum, r);
+    const ChunkRow to(p, it, it.row0 + r, g, cr.L, cr.n);
+    if (!to.live) continue;
+    const int at = r * (kHeadDim + 4) + 4 * col;
+    const f32x4 y = (*(f32x4 *)&lds_o[0][at] + *(f32x4 *)&lds_o[1][at]) * scale;
+    if (p.nsplit == 1) {
+      *(f32x4 *)((float *)p.out + to.at + 4 * col) = y;
+    } else {
+      float *pp = p.part + (to.at / kHeadDim * p.nsplit + split) * kPartStride;
+      if (col == 0) {
+        pp[0] = rm;
+        pp[1] = rs;
+      }
+      *(f32x2 *)(pp + 2 + 4 * col) = f32x2{y[0], y[1]};
+      *(f32x2 *)(pp + 4 + 4 * col) = f32x2{y[2], y[3]};
     }
   }
 }
@@ -576,19 +613,19 @@ static int64_t chunk_tiles(const WindowParams &p, int rows) {
   return p.n_rows * p.G / rows + std::min<int64_t>(p.batch, p.n_rows);
 }
 
-// Calls with few rows split what they see over workgroups, so that about two
-// workgroups run on each of the 256 compute units, at least four tiles for
-// each.
+// Calls with few rows split what they see over workgroups: bfloat16 until two
+// workgroups run on each of the 256 compute units, with four tiles or more
+// each; float32, whose waves keep the matrix unit busy alone, until one does,
+// with a tile or more for each wave.
 void chunk_split(WindowParams &p, int kind, size_t scratch) {
   const bool f32 = kind == kCacheF32;
-  const int64_t keys = f32 ? kF32Keys * kWaves : kChunkKeys;
+  const int64_t keys = f32 ? kF32Keys * kWaves : 4 * kChunkKeys;   // of a workgroup, at least
   // (about as many row tiles: where sequences have less than one each, one)
   const int64_t seqs = std::min<int64_t>(p.batch, p.n_rows);
   const int64_t blocks =
       std::max(p.n_rows * p.G / (f32 ? kF32Rows : kChunkRows) + seqs / 2, seqs) * p.hkv;
-  int64_t seen = std::min<int64_t>(p.ncap, (int64_t)p.n_sink + p.window);
-  const int64_t most = seen / (4 * keys);
-  int64_t split = blocks > 0 ? 512 / blocks : 1;
+  const int64_t most = std::min<int64_t>(p.ncap, (int64_t)p.n_sink + p.window) / keys;
+  int64_t split = blocks > 0 ? (f32 ? 256 : 512) / blocks : 1;
   split = std::min<int64_t>(split, most);
   const int64_t row = (int64_t)(kPartStride * sizeof(float)) * p.hq * p.n_rows;
   split = std::min<int64_t>(split, row > 0 ? (int64_t)scratch / row : 1);
