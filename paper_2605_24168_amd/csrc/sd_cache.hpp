@@ -26,8 +26,9 @@ struct WindowParams {
   const int32_t *block_table;  // paged: [batch, max_pages]
   const int32_t *seq_lens;     // [batch]
   const int32_t *q_starts;     // [batch + 1]; null: one query per sequence
-  float *part;                 // [T * Hq][nsplit][kPartStride]: maximum in powers of two,
-                               // sum, 128 unnormalised channels of a split
+  float *part;                 // rows of kPartStride: maximum in powers of two, sum, 128
+                               // unnormalised channels of a split; packed queries: [T * Hq]
+                               // [nsplit] rows, else those of one workgroup after the other
   int64_t ncap;                // positions addressable per sequence
   int64_t n_rows;              // T
   int32_t n_pages;             // pages of the pool
@@ -35,14 +36,20 @@ struct WindowParams {
   int32_t batch, hq, hkv, G;
   int32_t n_sink, window;
   float scale2;                // softmax scale times log2(e)
-  int32_t span;                // tiles of 16 positions per split
-  int32_t nsplit;
-  int32_t quad;                // a workgroup takes four KV heads (one query per sequence)
+  int32_t nsplit;              // packed queries
+  // One query per sequence:
+  int64_t grid;                // workgroups
+  int32_t quad;                // a workgroup takes four KV heads
+  int32_t plans;               // ways to cut sequences to choose from (0: none is cut)
+  int32_t rounds[3];           // of workgroups on all compute units, for each of them
+  int32_t slots[3];            // their workgroups for each group of KV heads
 };
 
-// Splits of one sequence and KV head over workgroups, from what the host
-// knows (see window_split); fills p.span, p.nsplit and p.quad.
-void window_split(WindowParams &p, int kind, bool paged);
+// Workgroups of a call with one query per sequence, from what the host knows;
+// fills what follows `nsplit` above.  Their partials take at most `scratch`
+// bytes.
+void window_split(WindowParams &p, int kind, bool paged, size_t scratch);
+size_t token_part_bytes(const WindowParams &p);
 // The same for packed queries, with partials of at most `scratch` bytes; fills
 // p.nsplit.
 void chunk_split(WindowParams &p, int kind, size_t scratch);
@@ -94,7 +101,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 
 // A row's partials joined by one wave: lane l gets channels 2l and 2l + 1 of
-// the n splits at pp, divided by their sum.  Each lane takes a split's maximum
+// the n splits at pp, `step` floats apart, divided by their sum.  Each lane takes a split's maximum
 // and sum, so that their loads are under way together.
 struct Joined {
   float x, y;
@@ -110,28 +117,27 @@ __device__ __forceinline__ float get_partial(const float *at) {
   return *at;
 }
 template <bool SHARED>
-__device__ __forceinline__ Joined join_splits(const float *pp, int n) {
+__device__ __forceinline__ Joined join_splits(const float *pp, int64_t step, int n) {
   const int l = lane_id();
   float m = -3e38f;
-  for (int s = l; s < n; s += 64) m = fmaxf(m, get_partial<SHARED>(pp + (int64_t)s * kPartStride));
+  for (int s = l; s < n; s += 64) m = fmaxf(m, get_partial<SHARED>(pp + s * step));
   const float M = wave_max(m);
   float sum = 0.f, x = 0.f, y = 0.f;
   for (int s0 = 0; s0 < n; s0 += 64) {
     const int s = s0 + l;
     float f = 0.f;
     if (s < n) {
-      f = __builtin_amdgcn_exp2f(get_partial<SHARED>(pp + (int64_t)s * kPartStride) - M);
-      sum += f * get_partial<SHARED>(pp + (int64_t)s * kPartStride + 1);
+      f = __builtin_amdgcn_exp2f(get_partial<SHARED>(pp + s * step) - M);
+      sum += f * get_partial<SHARED>(pp + s * step + 1);
     }
     const int k = n - s0 < 64 ? n - s0 : 64;
-    const float *o = pp + (int64_t)s0 * kPartStride + 2 + 2 * l;
+    const float *o = pp + s0 * step + 2 + 2 * l;
     for (int i0 = 0; i0 < k; i0 += 8) {  // eight loads under way together
       float2 v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int64_t j = i0 + i < k ? i0 + i : k - 1;
-        v[i] = float2{get_partial<SHARED>(o + j * kPartStride),
-                      get_partial<SHARED>(o + j * kPartStride + 1)};
+        v[i] = float2{get_partial<SHARED>(o + j * step), get_partial<SHARED>(o + j * step + 1)};
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -139,7 +139,7 @@ __device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, int &
 }
 
 // ---------------------------------------------------------------------------
-// float32: bound by the matrix unit, at an eighth of its bfloat16 rate, so
+// float32: bound by the matrix unit, at a sixteenth of its bfloat16 rate, so
 // operands come straight from global memory.  The four waves of a workgroup
 // share 32 rows and take every fourth tile of 32 positions each; they join at
 // the end.  Keys and values pass through the same registers: each group of
@@ -599,7 +599,8 @@ __global__ __launch_bounds__(kBlock) void k_chunk_merge(WindowParams p) {
   const int l = lane_id();
   const ChunkRow row(p, it, it.row0 + __builtin_amdgcn_readfirstlane(wave_id()), g, 0, 0);
   if (!row.live) return;
-  const Joined v = join_splits<false>(p.part + row.at / kHeadDim * p.nsplit * kPartStride, p.nsplit);
+  const Joined v = join_splits<false>(p.part + row.at / kHeadDim * p.nsplit * kPartStride,
+                                      kPartStride, p.nsplit);
   if (F32) *(float2 *)((float *)p.out + row.at + 2 * l) = float2{v.x, v.y};
   else *(uint32_t *)((uint16_t *)p.out + row.at + 2 * l) = pack2(v.x, v.y);
 }

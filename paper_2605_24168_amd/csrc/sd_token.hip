@@ -7,8 +7,8 @@
 // bfloat16, 136 in 4 bits.
 //
 // A wave takes tiles of 16 positions, two at a time, straight from global
-// memory into the operand registers of the matrix unit; no LDS is touched
-// until the end.  With K the first operand, S = K q^T leaves lane (head =
+// memory into the operand registers of the matrix unit, by buffer loads whose
+// bounds are the tile's; no LDS is touched until the end.  With K the first operand, S = K q^T leaves lane (head =
 // lane & 15, quarter = lane >> 4) the scores of positions 4 r + quarter of its
 // tile, r = 0..3 (see row_of).  The weights p = 2^(scale (s - m)) then are, without any
 // move between lanes, the second operand of O^T = V^T p^T over the two tiles,
@@ -17,12 +17,14 @@
 // the second, and V's rows are loaded in that order.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "sd_cache.hpp"
 #include "sd_internal.hpp"
 
 namespace sd {
 
-constexpr int kUnits = 256;          // compute units of the chip
+constexpr int kUnits = 256;          // compute units of the chip; a workgroup fills one
 constexpr float kFloor = -1e30f;     // running maximum before the first position
 constexpr float kSlack = 8.f;        // a maximum moves once a score passes it by 2^8
 
@@ -94,52 +96,64 @@ __device__ __forceinline__ void load_query(const WindowParams &p, int b, int g, 
 // one instruction are then four rows in a run.
 __device__ __forceinline__ int row_of(int m) { return 4 * (m & 3) + (m >> 2); }
 
-// Byte offsets of a lane's reads from the tile's first row (rows beyond `last`
-// replaced by it), `stride` rows apart.
+// Byte offsets of a lane's reads from the tile's first row, `stride` rows apart.
 template <int KIND>
 struct Offsets {
   static constexpr int kBytes = KIND == kCacheF32 ? 512 : (KIND == kCacheBf16 ? 256 : kQ4RowBytes);
   uint32_t k, v[4], ks, vs[4];
-  __device__ __forceinline__ Offsets(int stride, int last) {
+  __device__ __forceinline__ explicit Offsets(int stride) {
     const int l = lane_id(), m = l & 15, a = l >> 4;
-    const uint32_t kr = (uint32_t)(min(row_of(m), last) * stride);
+    const uint32_t kr = (uint32_t)(row_of(m) * stride);
     k = kr * kBytes + 16 * a;
     ks = kr * kQ4Scales + a;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const uint32_t vr = (uint32_t)(min(4 * r + a, last) * stride);
+      const uint32_t vr = (uint32_t)((4 * r + a) * stride);
       v[r] = vr * kBytes + (KIND == kCacheQ4 ? 4 : 16) * m;
       vs[r] = vr * kQ4Scales;
     }
   }
 };
 
-// row0: the tile's first row, in units of rows.
+// Memory from `base` on, of which the first `bytes` may be read: what lies
+// behind reads as zeros, without an access.
+typedef __amdgpu_buffer_rsrc_t Span;
+__device__ __forceinline__ Span span_of(const void *base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00020000);
+}
+constexpr int kNonTemporal = 2;
+__device__ __forceinline__ u32x4 load16(Span s, uint32_t at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s, at, 0, kNonTemporal));
+}
+
+// row0: the tile's first row, in units of rows, of which `rows` from there on
+// may be read.
 template <int KIND>
-__device__ __forceinline__ void load_tile(const WindowParams &p, int64_t row0, const Offsets<KIND> &o,
-                                          Tile<KIND> &t) {
-  const char *k = p.k + row0 * o.kBytes, *v = p.v + row0 * o.kBytes;
+__device__ __forceinline__ void load_tile(const WindowParams &p, int64_t row0, int rows,
+                                          const Offsets<KIND> &o, Tile<KIND> &t) {
+  const Span k = span_of(p.k + row0 * o.kBytes, rows * o.kBytes);
+  const Span v = span_of(p.v + row0 * o.kBytes, rows * o.kBytes);
   if constexpr (KIND == kCacheBf16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + o.k + 64 * i));
+    for (int i = 0; i < 4; ++i) t.k[i] = load16(k, o.k + 64 * i);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) t.v[r] = __builtin_nontemporal_load((const u32x4 *)(v + o.v[r]));
+    for (int r = 0; r < 4; ++r) t.v[r] = load16(v, o.v[r]);
   } else if constexpr (KIND == kCacheF32) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t.k[i] = __builtin_nontemporal_load((const u32x4 *)(k + o.k + 64 * i));
+    for (int i = 0; i < 8; ++i) t.k[i] = load16(k, o.k + 64 * i);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        t.v[r][j] = __builtin_nontemporal_load((const u32x4 *)(v + o.v[r] + 256 * j));
+      for (int j = 0; j < 2; ++j) t.v[r][j] = load16(v, o.v[r] + 256 * j);
   } else {
-    const uint8_t *ks = p.ks + row0 * kQ4Scales, *vs = p.vs + row0 * kQ4Scales;
-    t.k = __builtin_nontemporal_load((const u32x4 *)(k + o.k));
-    t.ks = (uint32_t)ks[o.ks];
+    const Span ks = span_of(p.ks + row0 * kQ4Scales, rows * kQ4Scales);
+    const Span vs = span_of(p.vs + row0 * kQ4Scales, rows * kQ4Scales);
+    t.k = load16(k, o.k);
+    t.ks = __builtin_amdgcn_raw_buffer_load_b8(ks, o.ks, 0, 0);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      t.v[r] = __builtin_nontemporal_load((const uint32_t *)(v + o.v[r]));
-      t.vs[r] = *(const uint32_t *)(vs + o.vs[r]);
+      t.v[r] = __builtin_amdgcn_raw_buffer_load_b32(v, o.v[r], 0, kNonTemporal);
+      t.vs[r] = __builtin_amdgcn_raw_buffer_load_b32(vs, o.vs[r], 0, 0);
     }
   }
 }
@@ -270,46 +284,150 @@ __device__ __forceinline__ void store_out(const WindowParams &p, int64_t at, flo
   else ((uint16_t *)p.out)[at] = f32_to_bf16_rne(x);
 }
 
-// Splits of a (sequence, KV head) that are done; 0 between calls.  Only calls
-// of fewer items than kSplitItems split.
-constexpr int kSplitItems = 512;
+// Parts of a (sequence, group of KV heads) that are done; 0 between calls.
+constexpr int kSplitItems = 4096;
 static __device__ uint32_t splits_done[kSplitItems];
 
-// grid: splits fastest, then KV heads, then sequences; where a position holds
-// the rows of all heads, the heads fastest, so that they are read at about the
-// same time.  HEADS: KV heads of a workgroup, each with NW / HEADS waves.  The waves of a
-// workgroup take the steps of two tiles in turn, each with the loads of its
-// next step under way while it computes.
+// Sequences are cut into parts so that every compute unit gets about the same:
+// of parts of one length, the shortest that the slots suffice for.  (The host
+// knows no lengths, so the workgroups work this out, 1 us of each.  Cut by the
+// table's capacity instead, uneven batches take longer: 24 contiguous sequences
+// of 100-32K 428 instead of 290 us, 128 on pages of 100-16K 1073 instead of 870,
+// 60 in 4 bits of 100-32K 314 instead of 219, and 3 of 64K, whose 264 parts were
+// eight too many for one round, 186 instead of 136.)
+constexpr int kPlanChunks = 4;                 // of 64 sequences
+constexpr int kPlanSeqs = 64 * kPlanChunks;
+// What a workgroup costs beside its tiles, in sixteenths of a step of its waves
+// (131 KB of rows and 4.8 us, or 35 KB and 1.3 us in 4 bits; 4 us beside it).
+template <int KIND>
+constexpr int kPartCost = KIND == kCacheQ4 ? 50 : 13;
+
+struct TokenPart {
+  int b, s, n;    // sequence, part, parts of the sequence
+  int first;      // the sequence's first slot
+  int span;       // tiles of a part
+};
+
+// x / d rounded up, for 0 < x, d < 2^18, with inv = 1 / d but for 2^-23 of it:
+// the half keeps the product further from every integer than its rounding moves it.
+__device__ __forceinline__ int parts_of(int x, int d, float inv) {
+  return (int)(((float)(x + d - 1) + 0.5f) * inv);
+}
+__device__ __forceinline__ float inverse(int d) { return __builtin_amdgcn_rcpf((float)d); }
+
+// What slot y computes; false: nothing.  Every wave finds out for itself.
+template <int STEP, int COST>
+__device__ __forceinline__ bool token_part(const WindowParams &p, int y, TokenPart &t) {
+  t = TokenPart{y, 0, 1, y, INT32_MAX / 2};
+  if (p.plans == 0) return true;   // a workgroup for each item
+  const int l = lane_id();
+  auto steps_of = [&](int b) {   // at least one
+    const int n = tile_range(clamp_len(p.seq_lens, b, p.ncap), p.n_sink, p.window).n;
+    return max(1, (n + STEP - 1) / STEP);
+  };
+  int units[kPlanChunks];   // steps of this lane's sequences
+  int total = 0, top = 1;
+  if (p.batch == 1) {
+    total = top = __builtin_amdgcn_readfirstlane(steps_of(0));
+  } else {
+#pragma unroll
+    for (int c = 0; c < kPlanChunks; ++c) {
+      units[c] = 0;
+      if (64 * c >= p.batch) continue;
+      if (64 * c + l < p.batch) units[c] = steps_of(64 * c + l);
+      total += __builtin_amdgcn_readlane(wave_incl_scan(units[c]), 63);
+      top = max(top, (int)wave_max_u32((uint32_t)units[c]));
+    }
+  }
+  int span = top, best = INT32_MAX;
+#pragma unroll 1
+  for (int i = 0; i < p.plans; ++i) {
+    const int slots = p.slots[i];
+    int lo;
+    if (total == top * p.batch) {   // sequences of one length
+      const int n = (int)(((float)slots + 0.5f) * inverse(p.batch));
+      lo = parts_of(top, n, inverse(n));
+    } else {
+      // Between what would do without rounding up each sequence's parts and
+      // what does with a part more for each, four steps of a bisection.
+      lo = max(1, (int)((float)total * inverse(slots) - 0.125f));
+      int hi = top;
+      if (slots > p.batch) hi = min(hi, (int)((float)total * inverse(slots - p.batch) + 0.125f) + 1);
+#pragma unroll 1
+      for (int j = 0; j < 4 && lo < hi; ++j) {
+        const int mid = (lo + hi) >> 1;
+        const float inv = inverse(mid);
+        int n = 0;
+#pragma unroll
+        for (int c = 0; c < kPlanChunks; ++c)
+          if (64 * c < p.batch)
+            n += __builtin_amdgcn_readlane(wave_incl_scan(units[c] ? parts_of(units[c], mid, inv) : 0), 63);
+        if (n <= slots) hi = mid;
+        else lo = mid + 1;
+      }
+      lo = hi;
+    }
+    const int cost = p.rounds[i] * (16 * lo + COST);
+    if (cost < best) {
+      best = cost;
+      span = lo;
+    }
+  }
+  const float inv = inverse(span);
+  t.span = span * STEP;
+  if (p.batch == 1) {
+    t = TokenPart{0, y, parts_of(top, span, inv), 0, span * STEP};
+    return y < t.n;
+  }
+  int before = 0;
+#pragma unroll
+  for (int c = 0; c < kPlanChunks; ++c) {
+    if (64 * c >= p.batch) break;
+    const int n = units[c] ? parts_of(units[c], span, inv) : 0, upto = wave_incl_scan(n);
+    const uint64_t hit = __ballot(y - before < upto);
+    if (hit) {
+      const int src = __ffsll((unsigned long long)hit) - 1;
+      t.b = 64 * c + src;
+      t.n = __builtin_amdgcn_readlane(n, src);
+      t.first = before + __builtin_amdgcn_readlane(upto, src) - t.n;
+      t.s = y - t.first;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// grid: KV heads fastest, so that the rows of a position are read at about the
+// same time, then slots.  HEADS: KV heads of a workgroup, each with NW / HEADS
+// waves.  The waves of a workgroup take the steps of two tiles in turn, each
+// with the loads of its next step under way while it computes.
 template <int KIND, bool PAGED, int NW, int HEADS>
 __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_attend(WindowParams p) {
   constexpr int NS = NW / HEADS;   // waves of a head
-  constexpr int kAhead = KIND == kCacheQ4 ? 2 : 1;   // steps under way beside the computed one
   extern __shared__ float lds[];
   constexpr bool kInside = PAGED && KIND != kCacheQ4;   // the heads lie inside a position
   const int l = lane_id(), a = l >> 4;
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), sub = w / HEADS;
   const uint32_t groups = p.hkv / HEADS;
-  const uint32_t n0 = kInside ? groups : p.nsplit, n1 = kInside ? p.nsplit : groups;
-  const uint32_t x0 = blockIdx.x % n0, x1 = blockIdx.x / n0;
-  const int b = (int)(x1 / n1);
-  const int s = (int)(kInside ? x1 % n1 : x0), g0 = HEADS * (int)(kInside ? x0 : x1 % n1);
-  const int g = g0 + w % HEADS;
+  const int g0 = HEADS * (int)(blockIdx.x % groups), g = g0 + w % HEADS;
+  TokenPart part;
+  if (!token_part<2 * NS, kPartCost<KIND>>(p, (int)(blockIdx.x / groups), part)) return;
+  const int b = part.b;
   const int L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, b, p.ncap));
   const TileRange tr = tile_range(L, p.n_sink, p.window);
-  const int nsp = (tr.n + p.span - 1) / p.span;  // splits of this sequence
-  if (s > 0 && s >= nsp) return;
   const int64_t orow = (int64_t)b * p.hq + (int64_t)g0 * p.G;   // of the workgroup's HEADS * G rows
   const int orows = HEADS * p.G;
-  if (nsp == 0) {
+  if (tr.n == 0) {
     for (int i = threadIdx.x; i < orows * kHeadDim; i += 64 * NW)
       store_out<KIND>(p, orow * kHeadDim + i, 0.f);
     return;
   }
-  const int t0 = s * p.span, t1 = min(tr.n, t0 + p.span);
+  const int t0 = part.s * part.span, t1 = min(tr.n, t0 + part.span);
 
   QRegs<KIND> qr;
   load_query<KIND>(p, b, g, qr);
-  const Offsets<KIND> offs(PAGED && KIND != kCacheQ4 ? p.hkv : 1, kTile - 1);
+  const Offsets<KIND> offs(kInside ? p.hkv : 1);
 
   float m = kFloor, ls = 0.f;  // of this lane's head; ls over its own positions
   f32x4 acc[8];
@@ -344,18 +462,20 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     for (int u = 0; u < 2; ++u) {
       const int t = tile_of(i, u);
       st.ok[u] = t < t1;
+      int64_t row0;
+      int rows;
       if (PAGED) {
         const int slot = 2 * (i & 31) + u;
         st.ok[u] = st.ok[u] && !(outside >> slot & 1);
         const int64_t page = __builtin_amdgcn_readlane(pages, slot);
-        load_tile<KIND>(p, KIND == kCacheQ4 ? (page * p.hkv + g) * kTile : page * kTile * p.hkv + g,
-                        offs, st.tile[u]);
+        row0 = kInside ? page * kTile * p.hkv + g : (page * p.hkv + g) * kTile;
+        rows = kInside ? kTile * p.hkv - g : kTile;
       } else {
-        const int first = st.ok[u] ? tr.tile(t) * kTile : 0, last = L - 1 - first;
-        const int64_t row0 = ((int64_t)b * p.hkv + g) * p.ncap + first;
-        if (last >= kTile - 1) load_tile<KIND>(p, row0, offs, st.tile[u]);
-        else load_tile<KIND>(p, row0, Offsets<KIND>(1, last), st.tile[u]);
+        const int first = tr.tile(t) * kTile;
+        row0 = ((int64_t)b * p.hkv + g) * p.ncap + first;
+        rows = min(kTile, L - first);
       }
+      load_tile<KIND>(p, st.ok[u] ? row0 : 0, st.ok[u] ? rows : 0, offs, st.tile[u]);
     }
   };
   auto compute = [&](int i, Step &st) {
@@ -405,23 +525,22 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     add_values<KIND>(acc, st.tile[0], st.tile[1], pw[0], pw[1]);
   };
 
-  Step st[kAhead + 1];
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d)
-    if (d < steps) {
-      hold_pages(d);
-      load(d, st[d]);
-    }
-  for (int i = 0; i < steps; i += kAhead + 1) {
-#pragma unroll
-    for (int d = 0; d <= kAhead; ++d) {
-      if (i + d >= steps) break;
-      if (i + d + kAhead < steps) {
-        hold_pages(i + d + kAhead);
-        load(i + d + kAhead, st[(d + kAhead) % (kAhead + 1)]);
-      }
-      compute(i + d, st[d]);
-    }
+  // (Loads past the last step touch no memory, and being unconditional let the
+  // waits count which ones are due.)
+  Step st[2];
+  hold_pages(0);
+  load(0, st[0]);
+  // (Loads past the last step touch no memory, and being unconditional let the
+  // waits count which ones are due.)
+  if (steps == 1) compute(0, st[0]);
+  for (int i = 0; steps > 1 && i < steps; i += 2) {
+    hold_pages(i + 1);
+    load(i + 1, st[1]);
+    compute(i, st[0]);
+    if (i + 1 >= steps) break;
+    hold_pages(i + 2);
+    load(i + 2, st[0]);
+    compute(i + 1, st[1]);
   }
 
   // Join the waves: per head a common maximum, scaled sums and outputs.
@@ -460,10 +579,10 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
       sum += f * ml[2 * row + 1];
       v += f * o[row * kRow + c];
     }
-    if (nsp == 1) {
+    if (part.n == 1) {
       store_out<KIND>(p, (orow + hh) * kHeadDim + c, sum == 0.f ? 0.f : v / sum);
     } else {
-      float *pp = p.part + ((orow + hh) * p.nsplit + s) * kPartStride;
+      float *pp = p.part + ((int64_t)blockIdx.x * orows + hh) * kPartStride;
       if (c == 0) {
         put_shared(pp, M);
         put_shared(pp + 1, sum);
@@ -471,7 +590,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
       put_shared(pp + 2 + c, v);
     }
   }
-  if (nsp == 1) return;
+  if (part.n == 1) return;
 
   // The workgroup that finishes last joins the splits, a wave per query head.
   // Each one counts itself once its partials have arrived where every compute
@@ -481,11 +600,13 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0)
-    *(uint32_t *)lds = atomicInc(&splits_done[x1 / n1 * groups + g0 / HEADS], (uint32_t)nsp - 1);
+    *(uint32_t *)lds = atomicInc(&splits_done[b * groups + g0 / HEADS], (uint32_t)part.n - 1);
   __syncthreads();
-  if (*(volatile uint32_t *)lds != (uint32_t)nsp - 1) return;
+  if (*(volatile uint32_t *)lds != (uint32_t)part.n - 1) return;
+  const int64_t first = (int64_t)part.first * groups + g0 / HEADS;   // the item's workgroups
   for (int hh = w; hh < orows; hh += NW) {
-    const Joined v = join_splits<true>(p.part + (orow + hh) * p.nsplit * kPartStride, nsp);
+    const Joined v = join_splits<true>(p.part + (first * orows + hh) * kPartStride,
+                                       (int64_t)groups * orows * kPartStride, part.n);
     const int64_t at = (orow + hh) * kHeadDim + 2 * l;
     store_out<KIND>(p, at, v.x);
     store_out<KIND>(p, at + 1, v.y);
@@ -500,43 +621,55 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
 static constexpr int token_waves(int kind) { return kind == kCacheF32 ? 4 : 8; }
 
 // Four KV heads to a workgroup pay on bfloat16 pages, whose rows of one head
-// are scattered 256-byte pieces, once there is enough to read and few splits
-// are needed: 64 sequences of 200-64K with a window of 4096 take 177 us instead
-// of 196, 16 of 16K 169 instead of 190, 16 of 4K 49 instead of 53; below, the
-// longer joins cost more (16 of 1K: 20 instead of 19; 4 of 16K: 55 instead of
-// 53; one of 64K: 80 instead of 54).
-constexpr int64_t kQuadItems = 128;     // sequences times KV heads
+// are scattered 256-byte pieces, once there is enough to read: 64 sequences
+// with a window of 4096 take 182 us instead of 204, 32 of 100-32K 376 instead
+// of 468, 8 of 32K 207 instead of 224; below, the longer joins cost more (32 of
+// 1K: 36 instead of 32; one of 64K: 85 instead of 59).
+constexpr int64_t kQuadItems = 64;      // sequences times KV heads
 constexpr int64_t kQuadTiles = 32768;   // the same times tiles
 
-void window_split(WindowParams &p, int kind, bool paged) {
+void window_split(WindowParams &p, int kind, bool paged, size_t scratch) {
   const int waves = token_waves(kind);
   const int64_t cap = (p.ncap + kTile - 1) / kTile;
   int64_t tiles = ((int64_t)p.n_sink + kTile - 1) / kTile + ((int64_t)p.window + kTile - 1) / kTile + 1;
-  if (tiles > cap) tiles = cap;
-  if (tiles < 1) tiles = 1;
+  tiles = std::min(tiles, cap);
   const int64_t all = (int64_t)p.batch * p.hkv;
   p.quad = paged && kind == kCacheBf16 && p.hkv % 4 == 0 && all >= kQuadItems &&
            all * tiles >= kQuadTiles;
   const int heads = p.quad ? 4 : 1;
-  const int64_t items = all / heads;
-  const int64_t step = 2 * waves / heads;
-  const int64_t target = 2 * kUnits * 4 / waves;
-  int64_t split = items > 0 ? (target + items - 1) / items : 1;
-  const int64_t most = (tiles + step - 1) / step;   // at least a step for each wave
-  split = split < 1 || items > kSplitItems ? 1 : (split > most ? most : split);
-  int64_t span = (tiles + split - 1) / split;
-  span = (span + step - 1) / step * step;
-  p.span = (int32_t)span;
-  p.nsplit = (int32_t)((tiles + span - 1) / span);
+  const int64_t items = all / heads, groups = p.hkv / heads;
+  const int64_t units = tiles * heads / (2 * waves);   // whole steps of a sequence, at most
+  const int64_t k0 = (items + kUnits - 1) / kUnits;
+  p.plans = 0;
+  p.grid = items;
+  if (units < 1 || items > kSplitItems || p.batch > kPlanSeqs) return;
+  // Plans of as many rounds of workgroups as the items need, one more, and
+  // twice as many: more balance better where each sequence has few parts in one
+  // round, and cost more where there is little to do.
+  const int64_t row = (int64_t)(kPartStride * sizeof(float)) * p.G * heads;
+  for (const int64_t k : {k0, k0 + 1, 2 * k0 + 1}) {
+    const int64_t slots = kUnits * k / groups;
+    if (slots * groups * row > (int64_t)scratch) break;
+    if (k == k0 + 1 && (p.batch * 4 <= p.slots[0] || p.batch * units < 8 * p.slots[0])) break;
+    p.slots[p.plans] = (int32_t)slots;
+    p.rounds[p.plans++] = (int32_t)k;
+  }
+  if (!p.plans || p.slots[p.plans - 1] <= p.batch) p.plans = 0;
+  else p.grid = p.slots[p.plans - 1] * groups;
+}
+
+// Bytes of partials (0: none).
+size_t token_part_bytes(const WindowParams &p) {
+  if (!p.plans) return 0;
+  return (size_t)p.grid * p.G * (p.quad ? 4 : 1) * kPartStride * sizeof(float);
 }
 
 template <int KIND, bool PAGED, int HEADS>
 static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
   constexpr int NW = token_waves(KIND);
-  const int64_t grid = (int64_t)p.batch * (p.hkv / HEADS) * p.nsplit;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (p.grid > INT32_MAX) return hipErrorInvalidConfiguration;
   k_token_attend<KIND, PAGED, NW, HEADS>
-      <<<(unsigned)grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
+      <<<(unsigned)p.grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
   return hipGetLastError();
 }
 

@@ -227,6 +227,16 @@ def test_attention_long_and_other_scales(sd):
     check_attention(sd, [300], 8, 2, "bhnd", seed=5, scale=1.0)
 
 
+@pytest.mark.parametrize("layout", ["bhnd", "paged"])
+@pytest.mark.parametrize("n,most,hq,hkv", [(2, 9000, 4, 1), (9, 5000, 8, 8), (65, 1500, 3, 1),
+                                           (200, 700, 2, 2)])
+def test_attention_over_very_different_lengths(sd, layout, n, most, hq, hkv):
+    lens = np.floor(np.exp(np.random.default_rng(n).uniform(0, np.log(most + 1), n))).astype(int) - 1
+    lens = [int(x) for x in lens] + [most]
+    check_attention(sd, lens, hq, hkv, layout, seed=n)
+    check_attention(sd, lens, hq, hkv, layout, 30, 500, seed=n)
+
+
 def test_attention_skips_pages_outside_the_pool(sd):
     def change(c):
         c.block_table[0, 0], c.block_table[1, 5] = c.k.shape[0], -3

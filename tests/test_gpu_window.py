@@ -9,6 +9,7 @@ from tests import plain64 as R
 
 pytestmark = pytest.mark.gpu
 SCALE = 128**-0.5
+ALL = 2**31 - 1
 
 
 @pytest.fixture(scope="module")
@@ -228,6 +229,36 @@ def test_without_a_window_only_the_first_tokens_are_read(sd, dtype):
             pr.cache.k[0, :, 5:300] = bad
             pr.cache.v[0, :, 5:300] = bad
             pr.check(pr.run(sd.Window(5, 0), counts is not None), 5, 0)
+
+
+def uneven(n, most, seed):
+    """n lengths from 0 to most, log-uniform."""
+    x = np.random.default_rng(seed).uniform(0, np.log(most + 1), n)
+    lens = np.floor(np.exp(x)).astype(int) - 1
+    lens[n // 2] = most
+    return [int(v) for v in lens]
+
+
+@pytest.mark.parametrize("layout", ["bhnd", "paged"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,most,hq,hkv", [(2, 9000, 4, 1), (9, 5000, 8, 8), (17, 3000, 4, 4),
+                                           (65, 1500, 3, 1), (130, 700, 2, 2), (256, 400, 1, 1),
+                                           (257, 400, 1, 1)])
+def test_sequences_of_very_different_lengths(sd, layout, dtype, n, most, hq, hkv):
+    # (cut into parts by a plan over all lengths, 64 sequences at a time)
+    pr = Problem(sd, uneven(n, most, n), hq, hkv, layout, dtype, seed=n, cap=2 * most)
+    for sink, window in ((0, ALL), (40, 600)):
+        pr.check(pr.run(sd.Window(sink, window), False), sink, window)
+    same = Problem(sd, [most // 4] * n, hq, hkv, layout, dtype, seed=n + 1)
+    same.check(same.run(sd.Window(), False), 0, ALL)
+
+
+def test_pages_of_four_heads_to_a_workgroup(sd):
+    # (enough heads, sequences and tiles for the variant: 64 x 4 x 150)
+    pr = Problem(sd, uneven(64, 2399, 3), 8, 4, "paged", "bf16", seed=19)
+    pr.check(pr.run(sd.Window(), False), 0, ALL)
+    pr = Problem(sd, [2390 - i for i in range(64)], 4, 4, "paged", "bf16", seed=20)
+    pr.check(pr.run(sd.Window(33, 2300), False), 33, 2300)
 
 
 @pytest.mark.parametrize("layout", ["bhnd", "paged"])
