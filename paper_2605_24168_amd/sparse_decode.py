@@ -694,58 +694,114 @@ def _int32(x, name: str) -> int:
     return x
 
 
-def _q4_descs(cache: Q4Cache) -> tuple:
+# Descriptors of the calls below, of tensors that have to be on device `index`.
+# What is as it should be takes one look at each property (a call's tensors cost
+# 0.3 us of host time each); everything else goes on to the checks that raise.
+_I32 = torch.int32
+_PACK_ROWS = struct.Struct("@Pii3q8x").pack      # an sd_tensor of three dimensions
+
+
+def _device_of(t: torch.Tensor, name: str) -> int:
+    index = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if index < 0:
+        _need_device(t, name)  # raises
+    return index
+
+
+def _same_device(t: torch.Tensor, name: str, index: int) -> None:
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the call on device {index}")
+
+
+def _rows_desc(t: torch.Tensor, name: str, index: int) -> bytes:
+    """[rows, heads, channels]"""
+    try:
+        if t.get_device() == index and t.is_contiguous():
+            shape = t.shape
+            if len(shape) == 3:
+                return _PACK_ROWS(t.data_ptr(), _DTYPES[t.dtype], 3, *shape)
+    except (AttributeError, KeyError):
+        pass
+    desc = _desc(t, name)
+    _same_device(t, name, index)
+    return desc
+
+
+def _pool_fields(t: torch.Tensor, name: str, index: int, dtypes) -> tuple:
+    """_fields of a cache's tensor."""
+    try:
+        if t.get_device() == index and t.is_contiguous():
+            shape = t.shape
+            if len(shape) == 4:
+                return t.data_ptr(), dtypes[t.dtype], 4, *shape
+    except (AttributeError, KeyError):
+        pass
+    fields = _fields(t, name, dtypes)
+    _same_device(t, name, index)
+    return fields
+
+
+def _vector(t: torch.Tensor, name: str, index: int, n: Optional[int] = None) -> int:
+    """Address of an int32 vector (of n entries)."""
+    try:
+        if t.get_device() == index and t.dtype is _I32 and t.is_contiguous() and \
+                t.dim() == 1 and (n is None or t.shape[0] == n):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _need_device(t, name, _I32)
+    _same_device(t, name, index)
+    raise ValueError(f"{name} must have the shape [{'n' if n is None else n}]")
+
+
+def _places(cache, batch: int, index: int) -> tuple:
+    """What a cache's descriptors hold beside its tensors."""
     if cache.layout == "paged":
         bt = cache.block_table
-        _need_device(bt, "block_table", torch.int32)
-        tail = (SD_KV_PAGED_NHD, cache.page_size & _U32, bt.data_ptr(), bt.shape[1])
-    elif cache.layout == "bhnd":
-        tail = (SD_KV_BHND, 0, 0, 0)
-    else:
-        raise ValueError(f"unknown layout {cache.layout!r}")
-    return tuple(_PACK_KV4.pack(*_fields(codes, name, _DTYPES_U8),
-                                *_fields(scales, name + "_scales", _DTYPES_U8), *tail)
-                 for name, codes, scales in (("k", cache.k, cache.k_scales),
-                                             ("v", cache.v, cache.v_scales)))
-
-
-def _empty_like(q: torch.Tensor, stream) -> torch.Tensor:
-    if stream is None and q.is_contiguous():
-        return torch.empty_like(q)
-    return _empty(q.shape, q.dtype, q.device, stream)
-
-
-def _need_vector(t: torch.Tensor, name: str, n: Optional[int] = None) -> None:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.int32 or \
-            not t.is_contiguous():
-        _need_device(t, name, torch.int32)  # raises
-    if t.dim() != 1 or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name} must have the shape [{'n' if n is None else n}]")
-
-
-def _batch_of(cache, seq_lens, starts) -> int:
-    """Sequences of a call; checks seq_lens, starts and the block table."""
-    _need_vector(seq_lens, "seq_lens")
-    batch = int(seq_lens.shape[0])
-    if starts is not None:
-        _need_vector(starts, "starts", batch + 1)
-    if cache.layout == "paged" and (cache.block_table is None or cache.block_table.dim() != 2 or
-                                    cache.block_table.shape[0] != batch):
+        try:
+            if bt.get_device() == index and bt.dtype is _I32 and bt.is_contiguous():
+                shape = bt.shape
+                if len(shape) == 2 and shape[0] == batch:
+                    return SD_KV_PAGED_NHD, cache.page_size & _U32, bt.data_ptr(), shape[1]
+        except AttributeError:
+            pass
+        _need_device(bt, "block_table", _I32)
+        _same_device(bt, "block_table", index)
         raise ValueError(f"block_table must have the shape [{batch}, max_pages]")
-    return batch
+    if cache.layout != "bhnd":
+        raise ValueError(f"unknown layout {cache.layout!r}")
+    return SD_KV_BHND, 0, 0, 0
 
 
-def _same_device(first: torch.Tensor, *others) -> None:
-    index = first.get_device()
-    for t in others:
-        if t is not None and t.get_device() != index:
-            raise ValueError(f"tensors on {first.device} and {t.device}")
+def _kv_descs(cache: KVCache, batch: int, index: int) -> tuple:
+    tail = _places(cache, batch, index)
+    return (_PACK_KV.pack(*_pool_fields(cache.k, "k", index, _DTYPES), *tail),
+            _PACK_KV.pack(*_pool_fields(cache.v, "v", index, _DTYPES), *tail))
+
+
+def _q4_descs(cache: Q4Cache, batch: int, index: int) -> tuple:
+    tail = _places(cache, batch, index)
+    return (_PACK_KV4.pack(*_pool_fields(cache.k, "k", index, _DTYPES_U8),
+                           *_pool_fields(cache.k_scales, "k_scales", index, _DTYPES_U8), *tail),
+            _PACK_KV4.pack(*_pool_fields(cache.v, "v", index, _DTYPES_U8),
+                           *_pool_fields(cache.v_scales, "v_scales", index, _DTYPES_U8), *tail))
+
+
+def _batch_of(seq_lens: torch.Tensor, index: int) -> tuple:
+    """Sequences of a call, and where their lengths are."""
+    at = _vector(seq_lens, "seq_lens", index)
+    return seq_lens.shape[0], at
+
+
+def _starts(starts, name: str, batch: int, index: int) -> Optional[int]:
+    return None if starts is None else _vector(starts, name, index, batch + 1)
 
 
 def _call(fn, index: int, stream, *args) -> None:
     """One library call on device `index`, with the stream appended."""
     if index == torch._C._cuda_getDevice():
-        status = fn(*args, _stream(stream))
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None
+                    else _stream(stream))
     else:
         with torch.cuda.device(index):
             status = fn(*args, _stream(stream))
@@ -753,18 +809,24 @@ def _call(fn, index: int, stream, *args) -> None:
         _check(status, fn.__name__)
 
 
-def _empty(shape, dtype, device, stream) -> torch.Tensor:
-    """An output, from the memory of the stream that the call runs on (on the
-    device's current stream without one)."""
+def _empty(like: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+    """An output on the device of `like`, from the memory of the stream that the
+    call runs on (the device's current stream without one)."""
     if stream is None:
-        if device.index == torch._C._cuda_getDevice():
-            return torch.empty(shape, dtype=dtype, device=device)
-        with torch.cuda.device(device):
-            return torch.empty(shape, dtype=dtype, device=device)
+        if like.get_device() == torch._C._cuda_getDevice():
+            return like.new_empty(shape, dtype=dtype)
+        with torch.cuda.device(like.device):
+            return like.new_empty(shape, dtype=dtype)
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(_stream(stream), device=device)
+        stream = torch.cuda.ExternalStream(_stream(stream), device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _empty_like(q: torch.Tensor, stream) -> torch.Tensor:
+    if stream is None and q.is_contiguous() and q.get_device() == torch._C._cuda_getDevice():
+        return torch.empty_like(q)
+    return _empty(q, q.shape, q.dtype, stream)
 
 
 def sparse_decode_window_attention(q, cache: KVCache, seq_lens, window: Window, q_starts=None,
@@ -774,13 +836,14 @@ def sparse_decode_window_attention(q, cache: KVCache, seq_lens, window: Window, 
     q_starts (int32 [B + 1]) sequence b's last positions as the rows
     q_starts[b] .. q_starts[b + 1] of q [T, Hq, 128].  Rows of no sequence
     are left as they are in `out` (unset without one)."""
-    batch = _batch_of(cache, seq_lens, q_starts)
+    index = _device_of(q, "q")
+    batch, lens = _batch_of(seq_lens, index)
+    starts = _starts(q_starts, "q_starts", batch, index)
     if out is None:
         out = _empty_like(q, stream)
-    _same_device(q, cache.k, cache.v, cache.block_table, seq_lens, q_starts, out)
-    cq, (kk, kv), co = _desc(q, "q"), _kv_desc(cache, "k", "v"), _desc(out, "out")
-    _call(_raw.sparse_decode_window_attention, q.get_device(), stream, cq, kk, kv,
-          seq_lens.data_ptr(), q_starts.data_ptr() if q_starts is not None else None, batch,
+    cq, co = _rows_desc(q, "q", index), _rows_desc(out, "out", index)
+    kk, kv = _kv_descs(cache, batch, index)
+    _call(_raw.sparse_decode_window_attention, index, stream, cq, kk, kv, lens, starts, batch,
           _window_desc(window), co)
     return out
 
@@ -789,11 +852,12 @@ def sparse_decode_q4_append(k, v, cache: Q4Cache, seq_lens, starts=None, stream=
     """Write the rows of k and v [T, Hkv, 128] as the last positions of their
     sequences (seq_lens counts them): row b of sequence b, or with starts
     (int32 [B + 1]) the rows starts[b] .. starts[b + 1]."""
-    batch = _batch_of(cache, seq_lens, starts)
-    _same_device(k, v, *cache.pools, cache.block_table, seq_lens, starts)
-    ck, cv, (kk, kv) = _desc(k, "k"), _desc(v, "v"), _q4_descs(cache)
-    _call(_raw.sparse_decode_q4_append, k.get_device(), stream, ck, cv, kk, kv, seq_lens.data_ptr(),
-          starts.data_ptr() if starts is not None else None, batch)
+    index = _device_of(k, "k")
+    batch, lens = _batch_of(seq_lens, index)
+    starts = _starts(starts, "starts", batch, index)
+    ck, cv = _rows_desc(k, "k", index), _rows_desc(v, "v", index)
+    kk, kv = _q4_descs(cache, batch, index)
+    _call(_raw.sparse_decode_q4_append, index, stream, ck, cv, kk, kv, lens, starts, batch)
 
 
 def sparse_decode_q4_load(cache: Q4Cache, seq_lens, starts=None, tokens: Optional[int] = None,
@@ -802,19 +866,23 @@ def sparse_decode_q4_load(cache: Q4Cache, seq_lens, starts=None, tokens: Optiona
     and v [T, Hkv, 128], rows as in sparse_decode_q4_append (tokens = T, when
     k and v are not given and starts is).  Rows of no sequence are left as
     they are (unset in new tensors)."""
-    batch = _batch_of(cache, seq_lens, starts)
+    index = _device_of(cache.k, "cache.k")
+    batch, lens = _batch_of(seq_lens, index)
     if (k is None or v is None) and tokens is None:
         if starts is not None:
             raise ValueError("tokens: the rows of k and v must be given beside starts")
         tokens = batch
+    starts = _starts(starts, "starts", batch, index)
+    kk, kv = _q4_descs(cache, batch, index)
     shape = (tokens, cache.num_kv_heads, 128)
-    dev = cache.k.device
-    k = _empty(shape, dtype, dev, stream) if k is None else k
-    v = _empty(shape, dtype, dev, stream) if v is None else v
-    _same_device(k, v, *cache.pools, cache.block_table, seq_lens, starts)
-    ck, cv, (kk, kv) = _desc(k, "k"), _desc(v, "v"), _q4_descs(cache)
-    _call(_raw.sparse_decode_q4_load, k.get_device(), stream, kk, kv, seq_lens.data_ptr(),
-          starts.data_ptr() if starts is not None else None, batch, ck, cv)
+    if k is None and v is None:
+        k = _empty(cache.k, shape, dtype, stream)
+        v = _empty_like(k, stream)
+    elif k is None or v is None:
+        new = _empty(cache.k, shape, dtype, stream)
+        k, v = (new, v) if k is None else (k, new)
+    ck, cv = _rows_desc(k, "k", index), _rows_desc(v, "v", index)
+    _call(_raw.sparse_decode_q4_load, index, stream, kk, kv, lens, starts, batch, ck, cv)
     return k, v
 
 
@@ -822,35 +890,35 @@ def sparse_decode_q4_attention(q, cache: Q4Cache, seq_lens, window: Optional[Win
                                out=None, stream=None):
     """Decode attention over a 4-bit cache (bfloat16 q [B, Hq, 128]): every
     position, or those that `window` leaves visible."""
-    _batch_of(cache, seq_lens, None)
-    if q.shape[0] != seq_lens.shape[0]:
+    index = _device_of(q, "q")
+    batch, lens = _batch_of(seq_lens, index)
+    if q.shape[0] != batch:
         raise ValueError("q and seq_lens must have the same number of sequences")
     if out is None:
         out = _empty_like(q, stream)
-    _same_device(q, *cache.pools, cache.block_table, seq_lens, out)
-    cq, (kk, kv), co = _desc(q, "q"), _q4_descs(cache), _desc(out, "out")
+    cq, co = _rows_desc(q, "q", index), _rows_desc(out, "out", index)
+    kk, kv = _q4_descs(cache, batch, index)
     cw = _window_desc(window) if window is not None else None
-    _call(_raw.sparse_decode_q4_attention, q.get_device(), stream, cq, kk, kv,
-          seq_lens.data_ptr(), cw, co)
+    _call(_raw.sparse_decode_q4_attention, index, stream, cq, kk, kv, lens, cw, co)
     return out
 
 
-def _pages_desc(pages: Pages) -> bytes:
+def _pages_desc(pages: Pages, index: int) -> bytes:
     bt = pages.block_table
-    _need_device(bt, "block_table", torch.int32)
-    if bt.dim() != 2:
+    if bt.dtype is not _I32 or not bt.is_contiguous():
+        _need_device(bt, "block_table", _I32)  # raises
+    shape = bt.shape
+    if len(shape) != 2:
         raise ValueError("block_table must have the shape [batch, max_pages]")
-    _need_vector(pages.seq_lens, "seq_lens", int(bt.shape[0]))
-    _need_vector(pages.refs, "refs")
-    _same_device(bt, pages.seq_lens, pages.refs)
-    return _PACK_PAGES.pack(bt.data_ptr(), pages.seq_lens.data_ptr(), pages.refs.data_ptr(),
-                            pages.refs.shape[0], bt.shape[0], bt.shape[1])
+    lens = _vector(pages.seq_lens, "seq_lens", index, shape[0])
+    refs = _vector(pages.refs, "refs", index)
+    return _PACK_PAGES.pack(bt.data_ptr(), lens, refs, pages.refs.shape[0], *shape)
 
 
-def _pools_desc(pools: Sequence[torch.Tensor], device) -> tuple:
+def _pools_desc(pools: Sequence[torch.Tensor], index: int) -> tuple:
     for t in pools:
-        if t.device != device:
-            raise ValueError(f"tensors on {device} and {t.device}")
+        _device_of(t, "pools")
+        _same_device(t, "pools", index)
     return b"".join(_PACK_TENSOR.pack(*_fields(t, "pools", _DTYPES_U8)) for t in pools), len(pools)
 
 
@@ -858,13 +926,13 @@ def sparse_decode_pages_extend(pages: Pages, grow, status=None, stream=None):
     """Pages for grow[b] more positions of each row (int32 [B]), the lowest
     free ones first; seq_lens grows.  Returns status int32 [B]: 0 done, 1 no
     free pages left, 2 longer than the table; such rows stay as they are."""
-    cp, batch, dev = _pages_desc(pages), int(pages.block_table.shape[0]), pages.block_table.device
-    _need_vector(grow, "grow", batch)
-    status = _empty((batch,), torch.int32, dev, stream) if status is None else status
-    _need_vector(status, "status", batch)
-    _same_device(pages.block_table, grow, status)
-    _call(_raw.sparse_decode_pages_extend, dev.index, stream, cp, grow.data_ptr(),
-          status.data_ptr())
+    index = _device_of(pages.block_table, "block_table")
+    cp, batch = _pages_desc(pages, index), pages.block_table.shape[0]
+    at = _vector(grow, "grow", index, batch)
+    if status is None:
+        status = _empty(grow, (batch,), _I32, stream)
+    _call(_raw.sparse_decode_pages_extend, index, stream, cp, at,
+          _vector(status, "status", index, batch))
     return status
 
 
@@ -874,36 +942,34 @@ def sparse_decode_pages_fork(pages: Pages, to: Pages, parents, pools: Sequence[t
     outside its rows: an empty row): full pages are shared, a part-filled last
     page is copied in every pool.  keep=False ends the parents' rows (a step
     of beam search).  Returns status int32: 0 done, 1 no free page left."""
-    cp, ct, dev = _pages_desc(pages), _pages_desc(to), pages.block_table.device
-    batch = int(to.block_table.shape[0])
-    _need_vector(parents, "parents", batch)
-    status = _empty((batch,), torch.int32, dev, stream) if status is None else status
-    _need_vector(status, "status", batch)
-    _same_device(pages.block_table, to.block_table, parents, status)
-    pl, n = _pools_desc(pools, dev)
-    _call(_raw.sparse_decode_pages_fork, dev.index, stream, cp, ct, parents.data_ptr(),
-          int(bool(keep)), pl, n, status.data_ptr())
+    index = _device_of(pages.block_table, "block_table")
+    if _device_of(to.block_table, "block_table") != index:
+        _same_device(to.block_table, "block_table", index)  # raises
+    cp, ct, batch = _pages_desc(pages, index), _pages_desc(to, index), to.block_table.shape[0]
+    at = _vector(parents, "parents", index, batch)
+    if status is None:
+        status = _empty(parents, (batch,), _I32, stream)
+    pl, n = _pools_desc(pools, index)
+    _call(_raw.sparse_decode_pages_fork, index, stream, cp, ct, at, int(bool(keep)), pl, n,
+          _vector(status, "status", index, batch))
     return status
 
 
 def sparse_decode_pages_free(pages: Pages, rows, stream=None) -> None:
     """The listed rows (int32) give back their pages and are left empty."""
-    cp = _pages_desc(pages)
-    _need_vector(rows, "rows")
-    _same_device(pages.block_table, rows)
-    _call(_raw.sparse_decode_pages_free, rows.get_device(), stream, cp, rows.data_ptr(),
-          rows.shape[0])
+    index = _device_of(pages.block_table, "block_table")
+    cp, at = _pages_desc(pages, index), _vector(rows, "rows", index)
+    _call(_raw.sparse_decode_pages_free, index, stream, cp, at, rows.shape[0])
 
 
 def sparse_decode_pages_copy(pools: Sequence[torch.Tensor], src, dst, stream=None) -> None:
     """Page dst[i] = page src[i] in every pool (int32; a page is not both a
     source and a destination, nor a destination twice)."""
-    _need_vector(src, "src")
-    _need_vector(dst, "dst", int(src.shape[0]))
-    _same_device(src, dst)
-    pl, n = _pools_desc(pools, src.device)
-    _call(_raw.sparse_decode_pages_copy, src.get_device(), stream, pl, n, src.data_ptr(),
-          dst.data_ptr(), src.shape[0])
+    index = _device_of(src, "src")
+    at, moves = _vector(src, "src", index), src.shape[0]
+    to = _vector(dst, "dst", index, moves)
+    pl, n = _pools_desc(pools, index)
+    _call(_raw.sparse_decode_pages_copy, index, stream, pl, n, at, to, moves)
 
 
 def sparse_decode_pages_compact(pages: Pages, pools: Sequence[torch.Tensor] = (), remap=None,
@@ -911,16 +977,13 @@ def sparse_decode_pages_compact(pages: Pages, pools: Sequence[torch.Tensor] = ()
     """Move the live pages to the front of the pools; table and refs follow.
     Returns (remap int32 [pages]: where each page is now, -1 if it was free;
     n_live int32 [1])."""
-    cp, dev = _pages_desc(pages), pages.block_table.device
-    n = int(pages.refs.shape[0])
-    remap = _empty((n,), torch.int32, dev, stream) if remap is None else remap
-    n_live = _empty((1,), torch.int32, dev, stream) if n_live is None else n_live
-    _need_vector(remap, "remap", n)
-    _need_vector(n_live, "n_live", 1)
-    _same_device(pages.block_table, remap, n_live)
-    pl, count = _pools_desc(pools, dev)
-    _call(_raw.sparse_decode_pages_compact, dev.index, stream, cp, pl, count, remap.data_ptr(),
-          n_live.data_ptr())
+    index = _device_of(pages.block_table, "block_table")
+    cp, n = _pages_desc(pages, index), pages.refs.shape[0]
+    remap = _empty(pages.refs, (n,), _I32, stream) if remap is None else remap
+    n_live = _empty(pages.refs, (1,), _I32, stream) if n_live is None else n_live
+    pl, count = _pools_desc(pools, index)
+    _call(_raw.sparse_decode_pages_compact, index, stream, cp, pl, count,
+          _vector(remap, "remap", index, n), _vector(n_live, "n_live", index, 1))
     return remap, n_live
 
 
