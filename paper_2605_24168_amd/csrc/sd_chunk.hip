@@ -542,8 +542,13 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
     bring_values(cr.t0, lds.v[0]);
     if (cr.t0 + 1 < cr.t1) bring_keys(cr.t0 + 1, lds.k[1]);
     __syncthreads();
-    scores(lds.k[0], sa);
-    settle(sa, cr.t0);
+    // A wave without rows only brings its share of the tiles (8 drafted tokens
+    // of each of 32 sequences over 4096 positions: 118 -> 103 us).
+    const bool idle = it.row0 + 32 * w >= it.rows;
+    if (!idle) {
+      scores(lds.k[0], sa);
+      settle(sa, cr.t0);
+    }
     __syncthreads();
     // Tile t's scores are in `now`: bring the tiles after it, score the next
     // one, and add this one's values.
@@ -551,9 +556,11 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
       if (t + 1 < cr.t1) bring_values(t + 1, lds.v[par ^ 1]);
       const bool ends = PAGED && t + 2 >= held + 16;   // the held pages end before tile t + 2
       if (t + 2 < cr.t1 && !ends) bring_keys(t + 2, lds.k[par]);
-      scores(lds.k[par ^ 1], next);   // (past the last tile: of an old one, unused)
-      add(lds.v[par], now);
-      if (t + 1 < cr.t1) settle(next, t + 1);
+      if (!idle) {
+        scores(lds.k[par ^ 1], next);   // (past the last tile: of an old one, unused)
+        add(lds.v[par], now);
+        if (t + 1 < cr.t1) settle(next, t + 1);
+      }
       if (t + 2 < cr.t1 && ends) {
         hold_pages(t + 2);
         bring_keys(t + 2, lds.k[par]);
