@@ -1274,19 +1274,15 @@ char *static_scratch(size_t bytes, sd_status &st) {
 // Splits, scratch and launches of a call.
 sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
   const bool packed = p.q_starts != nullptr;
-  size_t bytes = 0;
-  if (packed) {
-    sd::chunk_split(p, kind, kScratchBytes);
-    if (p.nsplit > 1) bytes = (size_t)p.n_rows * p.hq * p.nsplit * sd::kPartStride * sizeof(float);
-  } else {
-    sd::window_split(p, kind, paged, kScratchBytes);
-    bytes = sd::token_part_bytes(p);
-  }
+  if (packed) sd::chunk_split(p, kind, kScratchBytes);
+  else sd::window_split(p, kind, paged, kScratchBytes);
+  const size_t bytes = packed ? sd::chunk_part_bytes(p) : sd::token_part_bytes(p);
   std::lock_guard<std::mutex> lk(g_mu);
   if (bytes > 0) {
     sd_status st = SD_OK;
     p.part = (float *)static_scratch(bytes, st);
     if (st) return st;
+    if (packed) p.part_n = (int32_t *)(p.part + p.n_rows * p.hq * p.nsplit * sd::kPartStride);
   }
   return hip_status(packed ? sd::launch_chunk_attend(p, kind, paged, (hipStream_t)stream)
                            : sd::launch_token_attend(p, kind, paged, (hipStream_t)stream));

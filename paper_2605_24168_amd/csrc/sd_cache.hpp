@@ -27,8 +27,9 @@ struct WindowParams {
   const int32_t *seq_lens;     // [batch]
   const int32_t *q_starts;     // [batch + 1]; null: one query per sequence
   float *part;                 // rows of kPartStride: maximum in powers of two, sum, 128
-                               // unnormalised channels of a split; packed queries: [T * Hq]
+                               // unnormalised channels of a part; packed queries: [T * Hq]
                                // [nsplit] rows, else those of one workgroup after the other
+  int32_t *part_n;             // packed queries: [T * Hq] parts of a row
   int64_t ncap;                // positions addressable per sequence
   int64_t n_rows;              // T
   int32_t n_pages;             // pages of the pool
@@ -36,23 +37,22 @@ struct WindowParams {
   int32_t batch, hq, hkv, G;
   int32_t n_sink, window;
   float scale2;                // softmax scale times log2(e)
-  int32_t nsplit;              // packed queries
-  // One query per sequence:
   int64_t grid;                // workgroups
-  int32_t quad;                // a workgroup takes four KV heads
+  int32_t quad;                // a workgroup takes four KV heads (one query per sequence)
+  int32_t nsplit;              // parts of an item that there is room for
   int32_t plans;               // ways to cut sequences to choose from (0: none is cut)
   int32_t rounds[3];           // of workgroups on all compute units, for each of them
   int32_t slots[3];            // their workgroups for each group of KV heads
+  int32_t part_cost;           // of a workgroup beside its units, in sixteenths of one
 };
 
-// Workgroups of a call with one query per sequence, from what the host knows;
-// fills what follows `nsplit` above.  Their partials take at most `scratch`
-// bytes.
+// Workgroups of a call, from what the host knows: fills p.grid and what follows.
+// Partials take at most `scratch` bytes; part_bytes: those that they take (0: no
+// sequence is cut), and where they lie.
 void window_split(WindowParams &p, int kind, bool paged, size_t scratch);
-size_t token_part_bytes(const WindowParams &p);
-// The same for packed queries, with partials of at most `scratch` bytes; fills
-// p.nsplit.
 void chunk_split(WindowParams &p, int kind, size_t scratch);
+size_t token_part_bytes(const WindowParams &p);
+size_t chunk_part_bytes(const WindowParams &p);
 hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 

@@ -22,6 +22,7 @@
 
 #include "sd_cache.hpp"
 #include "sd_internal.hpp"
+#include "sd_plan.hpp"
 
 namespace sd {
 
@@ -41,6 +42,7 @@ struct ChunkItem {
   int row0;    // of the sequence's n * G rows
   int rows;    // n * G
   int start;   // the sequence's first row of q, in tokens
+  int s, n;    // part, parts of what the rows see
 };
 
 // Item i of the row tiles (ROWS rows) of all sequences in order; false past the
@@ -81,20 +83,13 @@ __device__ __forceinline__ u32x2 read_columns(const char *lds) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lds));
 }
 
-// What the rows [row0, row0 + ROWS) of a sequence see, as tiles of KEYS
-// positions: those of the first tokens, then those of the windows, [t0, t1) of
-// them for this split.
-template <int ROWS, int KEYS>
-struct ChunkRange {
-  int L, n;          // positions, queries of the sequence
-  int pmin, pmax;    // positions of the first and last row
+// What rows at the positions pmin .. pmax see, as tiles of KEYS positions: those
+// of the first tokens, then those of the windows.
+template <int KEYS>
+struct SeenTiles {
   int sink, lo;      // some row sees j < sink or j >= lo
-  int na, b0, t0, t1;
-  __device__ __forceinline__ ChunkRange(const WindowParams &p, const ChunkItem &it, int split) {
-    L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, it.b, p.ncap));
-    n = it.rows / p.G;
-    pmin = position(p, it, it.row0);
-    pmax = position(p, it, it.row0 + ROWS - 1);
+  int na, b0, n;     // tiles of the first tokens, first one of the windows, all
+  __device__ __forceinline__ SeenTiles(const WindowParams &p, int pmin, int pmax) {
     sink = min(p.n_sink, pmax + 1);
     lo = pmin + 1 > p.window ? pmin + 1 - p.window : 0;
     if (p.window == 0) lo = max(pmax + 1, 0);   // no window at all
@@ -102,9 +97,30 @@ struct ChunkRange {
     b0 = lo / KEYS;
     b0 = b0 < na ? na : b0;
     const int end = p.window > 0 && pmax >= 0 ? pmax / KEYS + 1 : 0;
-    const int nt = na + (end > b0 ? end - b0 : 0);
-    t0 = (int)((int64_t)nt * split / p.nsplit);
-    t1 = (int)((int64_t)nt * (split + 1) / p.nsplit);
+    n = na + (end > b0 ? end - b0 : 0);
+  }
+};
+
+// What the rows [row0, row0 + ROWS) of a sequence see, and of its tiles those
+// of one part, [t0, t1).
+template <int ROWS, int KEYS>
+struct ChunkRange {
+  int L, n;          // positions, queries of the sequence
+  int pmin, pmax;    // positions of the first and last row
+  int sink, lo;
+  int na, b0, t0, t1;
+  __device__ __forceinline__ ChunkRange(const WindowParams &p, const ChunkItem &it) {
+    L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, it.b, p.ncap));
+    n = it.rows / p.G;
+    pmin = position(p, it, it.row0);
+    pmax = position(p, it, it.row0 + ROWS - 1);
+    const SeenTiles<KEYS> seen(p, pmin, pmax);
+    sink = seen.sink;
+    lo = seen.lo;
+    na = seen.na;
+    b0 = seen.b0;
+    t0 = (int)((int64_t)seen.n * it.s / it.n);
+    t1 = (int)((int64_t)seen.n * (it.s + 1) / it.n);
   }
   __device__ __forceinline__ int position(const WindowParams &p, const ChunkItem &it, int row) const {
     return L - n + (int)((uint32_t)min(row, it.rows - 1) / (uint32_t)p.G);
@@ -128,14 +144,44 @@ struct ChunkRow {
   }
 };
 
-// (split, KV head, row tile) of a workgroup; false: no such rows.
-template <int ROWS>
-__device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, int &split, ChunkItem &it) {
-  uint32_t i = blockIdx.x;
-  g = (int)(i % (uint32_t)p.hkv);
-  i /= (uint32_t)p.hkv;
-  split = (int)(i % (uint32_t)p.nsplit);
-  return chunk_item<ROWS>(p, (int)(i / (uint32_t)p.nsplit), it);
+// KV head, row tile and part of a workgroup; false: no such rows.  UNIT: tiles of
+// KEYS positions in a unit of the plan, of which a part has LEAST.
+template <int ROWS, int KEYS, int UNIT, int LEAST>
+__device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, ChunkItem &it) {
+  g = (int)(blockIdx.x % (uint32_t)p.hkv);
+  const int y = (int)(blockIdx.x / (uint32_t)p.hkv);
+  it.s = 0;
+  it.n = 1;
+  if (p.plans == 0) return chunk_item<ROWS>(p, y, it);
+  auto queries = [&](int b, int &start) {
+    start = (int)clamp_start(p.q_starts, b, p.n_rows);
+    return max(0, (int)clamp_start(p.q_starts, b + 1, p.n_rows) - start);
+  };
+  // (Units of the last row tile; those before see as much, or less.)
+  auto units = [&](int b, int &items) {
+    int start;
+    const int n = queries(b, start);
+    items = (n * p.G + ROWS - 1) / ROWS;
+    const int L = clamp_len(p.seq_lens, b, p.ncap);
+    const SeenTiles<KEYS> seen(p, L - n + max(0, items - 1) * ROWS / p.G, L - 1);
+    return max(1, (seen.n + UNIT - 1) / UNIT);
+  };
+  Part part;
+  if (!find_part(p, y, LEAST, units, part)) return false;
+  it.b = part.b;
+  it.row0 = part.item * ROWS;
+  it.rows = queries(part.b, it.start) * p.G;
+  it.rows = __builtin_amdgcn_readfirstlane(it.rows);
+  it.start = __builtin_amdgcn_readfirstlane(it.start);
+  it.s = part.s;
+  it.n = part.n;
+  return true;
+}
+
+// Where a row's partial of this part goes.  The first part leaves their number.
+__device__ __forceinline__ float *chunk_part(const WindowParams &p, const ChunkItem &it, int64_t row) {
+  if (it.s == 0) p.part_n[row] = it.n;
+  return p.part + (row * p.nsplit + it.s) * kPartStride;
 }
 
 // ---------------------------------------------------------------------------
@@ -157,10 +203,10 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
   __shared__ float lds_q[kF32Rows * kHeadDim];          // [channel / 4][row][4]
   __shared__ float lds_o[2][kF32Rows * (kHeadDim + 4)];
   __shared__ float lds_ml[kWaves][kF32Rows][2];
-  int g, split;
+  int g;
   ChunkItem it;
-  if (!chunk_place<kF32Rows>(p, g, split, it)) return;
-  const ChunkRange<kF32Rows, kF32Keys> cr(p, it, split);
+  if (!chunk_place<kF32Rows, kF32Keys, kWaves, 1>(p, g, it)) return;
+  const ChunkRange<kF32Rows, kF32Keys> cr(p, it);
   const int l = lane_id(), col = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(wave_id());
   const ChunkRow row(p, it, it.row0 + col, g, cr.L, cr.n);
@@ -320,7 +366,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
   if (w < 2) each([&](int c, f32x4 x) { *(f32x4 *)(mine + c) = x + *(f32x4 *)(mine + c); });
   __syncthreads();
   // Whole rows, 32 lanes each.  (Lane `col` has that row's maximum and sum.)
-  const float inv = p.nsplit > 1 ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
+  const float inv = it.n > 1 ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = 2 * w + 8 * i + half;   // lanes r and r + 32 hold row r
@@ -329,10 +375,11 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
     if (!to.live) continue;
     const int at = r * (kHeadDim + 4) + 4 * col;
     const f32x4 y = (*(f32x4 *)&lds_o[0][at] + *(f32x4 *)&lds_o[1][at]) * scale;
-    if (p.nsplit == 1) {
+    if (p.plans > 0 && it.n == 1 && col == 0) p.part_n[to.at / kHeadDim] = 1;
+    if (it.n == 1) {
       *(f32x4 *)((float *)p.out + to.at + 4 * col) = y;
     } else {
-      float *pp = p.part + (to.at / kHeadDim * p.nsplit + split) * kPartStride;
+      float *pp = chunk_part(p, it, to.at / kHeadDim);
       if (col == 0) {
         pp[0] = rm;
         pp[1] = rs;
@@ -360,10 +407,10 @@ template <bool PAGED>
 __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
   extern __shared__ u32x4 lds_raw[];
   ChunkStage &lds = *(ChunkStage *)lds_raw;
-  int g, split;
+  int g;
   ChunkItem it;
-  if (!chunk_place<kChunkRows>(p, g, split, it)) return;
-  const ChunkRange<kChunkRows, kChunkKeys> cr(p, it, split);
+  if (!chunk_place<kChunkRows, kChunkKeys, 1, 4>(p, g, it)) return;
+  const ChunkRange<kChunkRows, kChunkKeys> cr(p, it);
   const int b = it.b;
   const int l = lane_id(), col = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(wave_id());
@@ -575,8 +622,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
 
   ls += __shfl_xor(ls, 32);
   if (!row.live) return;
-  if (p.nsplit > 1) {
-    float *pp = p.part + (row.at / kHeadDim * p.nsplit + split) * kPartStride;
+  if (p.plans > 0 && it.n == 1) p.part_n[row.at / kHeadDim] = 1;
+  if (it.n > 1) {
+    float *pp = chunk_part(p, it, row.at / kHeadDim);
     if (half == 0) {
       pp[0] = m;
       pp[1] = ls;
@@ -597,7 +645,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
                 pack2(acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv)};
 }
 
-// Joins the splits of one row for each wave.
+// Joins the parts of one row for each wave.
 template <bool F32>
 __global__ __launch_bounds__(kBlock) void k_chunk_merge(WindowParams p) {
   ChunkItem it;
@@ -606,8 +654,10 @@ __global__ __launch_bounds__(kBlock) void k_chunk_merge(WindowParams p) {
   const int l = lane_id();
   const ChunkRow row(p, it, it.row0 + __builtin_amdgcn_readfirstlane(wave_id()), g, 0, 0);
   if (!row.live) return;
-  const Joined v = join_splits<false>(p.part + row.at / kHeadDim * p.nsplit * kPartStride,
-                                      kPartStride, p.nsplit);
+  const int64_t at = row.at / kHeadDim;
+  const int n = min(__builtin_amdgcn_readfirstlane(p.part_n[at]), p.nsplit);
+  if (n <= 1) return;
+  const Joined v = join_splits<false>(p.part + at * p.nsplit * kPartStride, kPartStride, n);
   if (F32) *(float2 *)((float *)p.out + row.at + 2 * l) = float2{v.x, v.y};
   else *(uint32_t *)((uint16_t *)p.out + row.at + 2 * l) = pack2(v.x, v.y);
 }
@@ -621,35 +671,63 @@ static int64_t chunk_tiles(const WindowParams &p, int rows) {
   return p.n_rows * p.G / rows + std::min<int64_t>(p.batch, p.n_rows);
 }
 
-// Calls with few rows split what they see over workgroups: bfloat16 until two
-// workgroups run on each of the 256 compute units, with four tiles or more
-// each; float32, whose waves keep the matrix unit busy alone, until one does,
-// with a tile or more for each wave.
+// Calls with few rows cut what they see over workgroups.  In one round two
+// bfloat16 workgroups run on each of the 256 compute units, or one float32
+// workgroup, whose waves keep the matrix unit busy alone.  (With as many parts
+// for every row tile, uneven batches take longer: 4 drafted tokens of each of 16
+// sequences of 500-32K 240 instead of 176 us, 200 of each of 6 of 1-16K 222
+// instead of 185, float32 16 of each of 5 of 500-8K 106 instead of 89; even ones
+// are 1-5% shorter, 8 of each of 32 sequences of 4K 103 instead of 107.)
 void chunk_split(WindowParams &p, int kind, size_t scratch) {
   const bool f32 = kind == kCacheF32;
-  const int64_t keys = f32 ? kF32Keys * kWaves : 4 * kChunkKeys;   // of a workgroup, at least
+  const int64_t rows = f32 ? kF32Rows : kChunkRows, round = f32 ? 256 : 512;
+  const int64_t least = f32 ? kF32Keys * kWaves : 4 * kChunkKeys;   // positions of a part
+  const int64_t bound = chunk_tiles(p, (int)rows);
+  p.plans = 0;
+  p.nsplit = 1;
+  p.grid = bound * p.hkv;
   // (about as many row tiles: where sequences have less than one each, one)
   const int64_t seqs = std::min<int64_t>(p.batch, p.n_rows);
-  const int64_t blocks =
-      std::max(p.n_rows * p.G / (f32 ? kF32Rows : kChunkRows) + seqs / 2, seqs) * p.hkv;
-  const int64_t most = std::min<int64_t>(p.ncap, (int64_t)p.n_sink + p.window) / keys;
-  int64_t split = blocks > 0 ? (f32 ? 256 : 512) / blocks : 1;
-  split = std::min<int64_t>(split, most);
+  const int64_t tiles = std::max(p.n_rows * p.G / rows + seqs / 2, seqs);
+  const int64_t k0 = (tiles * p.hkv + round - 1) / round;
   const int64_t row = (int64_t)(kPartStride * sizeof(float)) * p.hq * p.n_rows;
-  split = std::min<int64_t>(split, row > 0 ? (int64_t)scratch / row : 1);
-  p.nsplit = (int32_t)std::max<int64_t>(split, 1);
+  int64_t parts = std::min<int64_t>(p.ncap, (int64_t)p.n_sink + p.window) / least;
+  parts = std::min(parts, (int64_t)scratch / (row + 4 * p.hq * p.n_rows));
+  if (k0 > 2 || parts < 2 || p.batch > kPlanSeqs) return;
+  // A workgroup costs 4 us beside its tiles, and its partials.
+  const int64_t fill = std::min<int64_t>(rows, p.n_rows * p.G / tiles);
+  p.part_cost = (int32_t)(f32 ? 16 : 32 + 112 * fill / rows);
+  // More rounds than the row tiles need balance better where sequences differ
+  // (not where all are longer than their windows) and have few parts in one.
+  const bool more = p.batch > 1 && (int64_t)p.n_sink + p.window > p.ncap / 4;
+  for (const int64_t k : {k0, k0 + 1}) {
+    const int64_t slots = std::max(round * k / p.hkv, bound);
+    if (k > k0 && (!more || tiles * 4 <= p.slots[0] || tiles * parts < 4 * p.slots[0])) break;
+    p.slots[p.plans] = (int32_t)slots;
+    p.rounds[p.plans++] = (int32_t)k;
+  }
+  p.nsplit = (int32_t)parts;
+  p.grid = p.slots[p.plans - 1] * (int64_t)p.hkv;
+  if (p.plans > 1 || p.slots[0] >= 2 * tiles) return;
+  p.plans = 0;
+  p.nsplit = 1;
+  p.grid = bound * p.hkv;
+}
+
+size_t chunk_part_bytes(const WindowParams &p) {
+  return p.plans ? (size_t)p.n_rows * p.hq * (p.nsplit * kPartStride * sizeof(float) + sizeof(int32_t)) : 0;
 }
 
 hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
   const bool f32 = kind == kCacheF32;
-  const int64_t grid = chunk_tiles(p, f32 ? kF32Rows : kChunkRows) * p.hkv * p.nsplit;
+  const int64_t grid = p.grid;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   if (f32 && paged) k_chunk_f32<true><<<(unsigned)grid, kBlock, 0, st>>>(p);
   else if (f32) k_chunk_f32<false><<<(unsigned)grid, kBlock, 0, st>>>(p);
   else if (paged) k_chunk_bf16<true><<<(unsigned)grid, kBlock, sizeof(ChunkStage), st>>>(p);
   else k_chunk_bf16<false><<<(unsigned)grid, kBlock, sizeof(ChunkStage), st>>>(p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.nsplit == 1) return e;
+  if (e != hipSuccess || p.plans == 0) return e;
   const unsigned merge = (unsigned)(chunk_tiles(p, kWaves) * p.hkv);
   if (f32) k_chunk_merge<true><<<merge, kBlock, 0, st>>>(p);
   else k_chunk_merge<false><<<merge, kBlock, 0, st>>>(p);

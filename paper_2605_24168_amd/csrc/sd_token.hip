@@ -21,6 +21,7 @@
 
 #include "sd_cache.hpp"
 #include "sd_internal.hpp"
+#include "sd_plan.hpp"
 
 namespace sd {
 
@@ -288,115 +289,9 @@ __device__ __forceinline__ void store_out(const WindowParams &p, int64_t at, flo
 constexpr int kSplitItems = 4096;
 static __device__ uint32_t splits_done[kSplitItems];
 
-// Sequences are cut into parts so that every compute unit gets about the same:
-// of parts of one length, the shortest that the slots suffice for.  (The host
-// knows no lengths, so the workgroups work this out, 1 us of each.  Cut by the
-// table's capacity instead, uneven batches take longer: 24 contiguous sequences
-// of 100-32K 428 instead of 290 us, 128 on pages of 100-16K 1073 instead of 870,
-// 60 in 4 bits of 100-32K 314 instead of 219, and 3 of 64K, whose 264 parts were
-// eight too many for one round, 186 instead of 136.)
-constexpr int kPlanChunks = 4;                 // of 64 sequences
-constexpr int kPlanSeqs = 64 * kPlanChunks;
 // What a workgroup costs beside its tiles, in sixteenths of a step of its waves
 // (131 KB of rows and 4.8 us, or 35 KB and 1.3 us in 4 bits; 4 us beside it).
-template <int KIND>
-constexpr int kPartCost = KIND == kCacheQ4 ? 50 : 13;
-
-struct TokenPart {
-  int b, s, n;    // sequence, part, parts of the sequence
-  int first;      // the sequence's first slot
-  int span;       // tiles of a part
-};
-
-// x / d rounded up, for 0 < x, d < 2^18, with inv = 1 / d but for 2^-23 of it:
-// the half keeps the product further from every integer than its rounding moves it.
-__device__ __forceinline__ int parts_of(int x, int d, float inv) {
-  return (int)(((float)(x + d - 1) + 0.5f) * inv);
-}
-__device__ __forceinline__ float inverse(int d) { return __builtin_amdgcn_rcpf((float)d); }
-
-// What slot y computes; false: nothing.  Every wave finds out for itself.
-template <int STEP, int COST>
-__device__ __forceinline__ bool token_part(const WindowParams &p, int y, TokenPart &t) {
-  t = TokenPart{y, 0, 1, y, INT32_MAX / 2};
-  if (p.plans == 0) return true;   // a workgroup for each item
-  const int l = lane_id();
-  auto steps_of = [&](int b) {   // at least one
-    const int n = tile_range(clamp_len(p.seq_lens, b, p.ncap), p.n_sink, p.window).n;
-    return max(1, (n + STEP - 1) / STEP);
-  };
-  int units[kPlanChunks];   // steps of this lane's sequences
-  int total = 0, top = 1;
-  if (p.batch == 1) {
-    total = top = __builtin_amdgcn_readfirstlane(steps_of(0));
-  } else {
-#pragma unroll
-    for (int c = 0; c < kPlanChunks; ++c) {
-      units[c] = 0;
-      if (64 * c >= p.batch) continue;
-      if (64 * c + l < p.batch) units[c] = steps_of(64 * c + l);
-      total += __builtin_amdgcn_readlane(wave_incl_scan(units[c]), 63);
-      top = max(top, (int)wave_max_u32((uint32_t)units[c]));
-    }
-  }
-  int span = top, best = INT32_MAX;
-#pragma unroll 1
-  for (int i = 0; i < p.plans; ++i) {
-    const int slots = p.slots[i];
-    int lo;
-    if (total == top * p.batch) {   // sequences of one length
-      const int n = (int)(((float)slots + 0.5f) * inverse(p.batch));
-      lo = parts_of(top, n, inverse(n));
-    } else {
-      // Between what would do without rounding up each sequence's parts and
-      // what does with a part more for each, four steps of a bisection.
-      lo = max(1, (int)((float)total * inverse(slots) - 0.125f));
-      int hi = top;
-      if (slots > p.batch) hi = min(hi, (int)((float)total * inverse(slots - p.batch) + 0.125f) + 1);
-#pragma unroll 1
-      for (int j = 0; j < 4 && lo < hi; ++j) {
-        const int mid = (lo + hi) >> 1;
-        const float inv = inverse(mid);
-        int n = 0;
-#pragma unroll
-        for (int c = 0; c < kPlanChunks; ++c)
-          if (64 * c < p.batch)
-            n += __builtin_amdgcn_readlane(wave_incl_scan(units[c] ? parts_of(units[c], mid, inv) : 0), 63);
-        if (n <= slots) hi = mid;
-        else lo = mid + 1;
-      }
-      lo = hi;
-    }
-    const int cost = p.rounds[i] * (16 * lo + COST);
-    if (cost < best) {
-      best = cost;
-      span = lo;
-    }
-  }
-  const float inv = inverse(span);
-  t.span = span * STEP;
-  if (p.batch == 1) {
-    t = TokenPart{0, y, parts_of(top, span, inv), 0, span * STEP};
-    return y < t.n;
-  }
-  int before = 0;
-#pragma unroll
-  for (int c = 0; c < kPlanChunks; ++c) {
-    if (64 * c >= p.batch) break;
-    const int n = units[c] ? parts_of(units[c], span, inv) : 0, upto = wave_incl_scan(n);
-    const uint64_t hit = __ballot(y - before < upto);
-    if (hit) {
-      const int src = __ffsll((unsigned long long)hit) - 1;
-      t.b = 64 * c + src;
-      t.n = __builtin_amdgcn_readlane(n, src);
-      t.first = before + __builtin_amdgcn_readlane(upto, src) - t.n;
-      t.s = y - t.first;
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
-  }
-  return false;
-}
+static constexpr int part_cost(int kind) { return kind == kCacheQ4 ? 50 : 13; }
 
 // grid: KV heads fastest, so that the rows of a position are read at about the
 // same time, then slots.  HEADS: KV heads of a workgroup, each with NW / HEADS
@@ -411,8 +306,22 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   const int w = __builtin_amdgcn_readfirstlane(wave_id()), sub = w / HEADS;
   const uint32_t groups = p.hkv / HEADS;
   const int g0 = HEADS * (int)(blockIdx.x % groups), g = g0 + w % HEADS;
-  TokenPart part;
-  if (!token_part<2 * NS, kPartCost<KIND>>(p, (int)(blockIdx.x / groups), part)) return;
+  // (Cut by the table's capacity instead of a plan over all lengths, uneven
+  // batches take longer: 24 contiguous sequences of 100-32K 428 instead of 290
+  // us, 128 on pages of 100-16K 1073 instead of 870, 60 in 4 bits of 100-32K 314
+  // instead of 219, and 3 of 64K, whose 264 parts were eight too many for one
+  // round, 186 instead of 136.)
+  constexpr int kStep = 2 * NS;   // tiles that the waves of a head take at once
+  const int y = (int)(blockIdx.x / groups);
+  Part part{y, 0, 0, 1, y, INT32_MAX / kStep};
+  if (p.plans > 0) {
+    auto steps = [&](int i, int &items) {
+      items = 1;
+      const int n = tile_range(clamp_len(p.seq_lens, i, p.ncap), p.n_sink, p.window).n;
+      return max(1, (n + kStep - 1) / kStep);
+    };
+    if (!find_part(p, y, 1, steps, part)) return;
+  }
   const int b = part.b;
   const int L = __builtin_amdgcn_readfirstlane(clamp_len(p.seq_lens, b, p.ncap));
   const TileRange tr = tile_range(L, p.n_sink, p.window);
@@ -423,7 +332,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
       store_out<KIND>(p, orow * kHeadDim + i, 0.f);
     return;
   }
-  const int t0 = part.s * part.span, t1 = min(tr.n, t0 + part.span);
+  const int t0 = part.s * part.span * kStep, t1 = min(tr.n, t0 + part.span * kStep);
 
   QRegs<KIND> qr;
   load_query<KIND>(p, b, g, qr);
@@ -642,15 +551,19 @@ void window_split(WindowParams &p, int kind, bool paged, size_t scratch) {
   const int64_t k0 = (items + kUnits - 1) / kUnits;
   p.plans = 0;
   p.grid = items;
+  p.nsplit = kPlanSeqs * kUnits;   // (parts of an item: any number has room)
+  p.part_cost = part_cost(kind);
   if (units < 1 || items > kSplitItems || p.batch > kPlanSeqs) return;
   // Plans of as many rounds of workgroups as the items need, one more, and
-  // twice as many: more balance better where each sequence has few parts in one
-  // round, and cost more where there is little to do.
+  // twice as many: more balance better where sequences differ (not where all are
+  // longer than their windows) and have few parts in one round, and cost more
+  // where there is little to do.
+  const bool more = (int64_t)p.n_sink + p.window > p.ncap / 4;
   const int64_t row = (int64_t)(kPartStride * sizeof(float)) * p.G * heads;
   for (const int64_t k : {k0, k0 + 1, 2 * k0 + 1}) {
     const int64_t slots = kUnits * k / groups;
     if (slots * groups * row > (int64_t)scratch) break;
-    if (k == k0 + 1 && (p.batch * 4 <= p.slots[0] || p.batch * units < 8 * p.slots[0])) break;
+    if (k > k0 && (!more || p.batch * 4 <= p.slots[0] || p.batch * units < 8 * p.slots[0])) break;
     p.slots[p.plans] = (int32_t)slots;
     p.rounds[p.plans++] = (int32_t)k;
   }

@@ -253,6 +253,23 @@ def test_sequences_of_very_different_lengths(sd, layout, dtype, n, most, hq, hkv
     same.check(same.run(sd.Window(), False), 0, ALL)
 
 
+@pytest.mark.parametrize("layout", ["bhnd", "paged"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,most,few,hq,hkv", [(2, 6000, 5, 4, 1), (5, 4000, 40, 8, 2), (1, 5000, 3, 6, 2),
+                                               (1, 4000, 130, 8, 2), (70, 1200, 3, 2, 1),
+                                               (200, 600, 2, 1, 1), (9, 3000, 70, 16, 1)])
+def test_chunks_of_sequences_of_very_different_lengths(sd, layout, dtype, n, most, few, hq, hkv):
+    # (few rows over long contexts, cut into parts by a plan over all lengths)
+    lens = uneven(n, most, 100 + n)
+    counts = [int(c) for c in np.random.default_rng(n).integers(0, few + 1, n)]
+    counts[n // 2] = few
+    pr = Problem(sd, lens, hq, hkv, layout, dtype, counts=counts, seed=n, cap=2 * most)
+    for sink, window in ((0, ALL), (40, most // 2)):
+        pr.check(pr.run(sd.Window(sink, window), True), sink, window)
+    same = Problem(sd, [most] * min(n, 20), hq, hkv, layout, dtype, counts=[few] * min(n, 20), seed=n + 1)
+    same.check(same.run(sd.Window(), True), 0, ALL)
+
+
 def test_pages_of_four_heads_to_a_workgroup(sd):
     # (enough heads, sequences and tiles for the variant: 64 x 4 x 150)
     pr = Problem(sd, uneven(64, 2399, 3), 8, 4, "paged", "bf16", seed=19)
