@@ -23,6 +23,9 @@ names follow the C ABI in include/sparse_decode.h:
     sparse_decode_pages_copy(pools, src, dst)
     sparse_decode_pages_compact(pages, pools)                -> (remap, n_live)
 
+Calls on one device share the library's memory: they (and replays of graphs that
+hold them) have to be ordered, on one stream or by events.
+
 Importing this module raises if the library has not been built; nothing here
 falls back to another implementation.
 """
