@@ -368,7 +368,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   };
   struct Step {
     Tile<KIND> tile[2];
-    bool ok[2];   // the tile is one of this split's and its page in the pool
+    bool ok[2];   // the tile is one of this part's and its page in the pool
   };
   auto load = [&](int i, Step &st) {
 #pragma unroll
