@@ -25,6 +25,12 @@ constexpr int kPlan = 1024;                       // threads that count and plan
 // pages extended: 14.7, 11.8 and 12.8 us with 4, 2 and 1).
 constexpr int kPerThread = 2;
 constexpr int kStretch = kPlan * kPerThread;      // pages counted by one workgroup
+// Pools of at most this many pages are handed out (or listed) by the workgroup
+// that plans, stretch after stretch; larger ones by the stretches' workgroups of
+// a second launch.  (2000 pages moved together in 26 us a call instead of 30,
+// 8192 in 27 instead of 30, but 16384 in 41 instead of 34; rows of 8032 pages
+// freed and extended in 15.5 instead of 18.)
+constexpr int kOneLaunch = 4 * kStretch;
 constexpr int64_t kPiece = 16 * 1024;             // bytes a workgroup copies at once
 constexpr int kMany = 1 << 29;                    // more than any number of pages
 
@@ -127,10 +133,38 @@ __device__ __forceinline__ int plan_bases(const PageWork &w, int *tmp) {
 // ---------------------------------------------------------------------------
 // extend
 // ---------------------------------------------------------------------------
+// Rows that get pages are those whose ranks end at or below the limit; their
+// ranks ascend, so a free page finds its row by bisection, in LDS where the
+// rows' first ranks fit (256 rows, 262144 pages: 7.7 instead of 10.6 us, with
+// four pages a thread).
+constexpr int kRowsLds = 4096;
+
+// Hands out the free pages of stretch s, the first of which has rank `base`.
+__device__ __forceinline__ void take_stretch(const PagesParams &p, const PageWork &w, int s, int base,
+                                             int limit, int *tmp, const int *first_lds) {
+  const bool local = p.batch <= kRowsLds;
+  const uint32_t mine = stretch_bits<false>(p, s);
+  int total;
+  int rank = base + block_excl_scan<kPlan>(__popc(mine), tmp, &total);  // (also a barrier)
+  for (uint32_t m = mine; m && rank < limit; m &= m - 1, ++rank) {
+    const int page = s * kStretch + threadIdx.x * kPerThread + __ffs(m) - 1;
+    int lo = 0, hi = p.batch;  // first row whose ranks start past this one
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if ((local ? first_lds[mid] : w.first[mid]) <= rank) lo = mid + 1;
+      else hi = mid;
+    }
+    const int b = lo - 1;
+    p.table[(int64_t)b * p.max_pages + w.have[b] + rank - (local ? first_lds[b] : w.first[b])] = page;
+    p.refs[page] = 1;
+  }
+}
+
 __global__ __launch_bounds__(kPlan) void k_extend_plan(PagesParams p, PageWork w,
                                                        const int32_t *grow, int32_t *status) {
   __shared__ int tmp[kPlan / 64];
   __shared__ int limit;
+  __shared__ int first_lds[kRowsLds];
   if (!count_stretch<false>(p, w, tmp)) return;
   const int nfree = plan_bases(w, tmp);
   if (threadIdx.x == 0) limit = 0;
@@ -158,19 +192,19 @@ __global__ __launch_bounds__(kPlan) void k_extend_plan(PagesParams p, PageWork w
       if (ok) p.seq_lens[b] = (int32_t)L;
       w.first[b] = first;
       w.have[b] = have;
+      if (b < kRowsLds) first_lds[b] = first;
       if (ok && need > 0) atomicMax(&limit, first + need);
     }
     before = min(before + total, kMany);
   }
   __syncthreads();
-  if (threadIdx.x == 0) w.scalar[kLimit] = limit;
+  if (p.n_pages <= kOneLaunch) {
+    for (int s = 0; s < (int)gridDim.x && w.base[s] < limit; ++s)
+      take_stretch(p, w, s, w.base[s], limit, tmp, first_lds);
+  } else if (threadIdx.x == 0) {
+    w.scalar[kLimit] = limit;
+  }
 }
-
-// Rows that get pages are those whose ranks end at or below the limit; their
-// ranks ascend, so a free page finds its row by bisection, in LDS where the
-// rows' first ranks fit (256 rows, 262144 pages: 7.7 instead of 10.6 us, with
-// four pages a thread).
-constexpr int kRowsLds = 4096;
 
 __global__ __launch_bounds__(kPlan) void k_extend_take(PagesParams p, PageWork w) {
   __shared__ int tmp[kPlan / 64];
@@ -178,24 +212,9 @@ __global__ __launch_bounds__(kPlan) void k_extend_take(PagesParams p, PageWork w
   const int limit = w.scalar[kLimit];
   const int base = w.base[blockIdx.x];
   if (base >= limit) return;
-  const bool local = p.batch <= kRowsLds;
-  if (local)
+  if (p.batch <= kRowsLds)
     for (int i = threadIdx.x; i < p.batch; i += kPlan) first_lds[i] = w.first[i];
-  const uint32_t mine = stretch_bits<false>(p, blockIdx.x);
-  int total;
-  int rank = base + block_excl_scan<kPlan>(__popc(mine), tmp, &total);  // (also a barrier)
-  for (uint32_t m = mine; m && rank < limit; m &= m - 1, ++rank) {
-    const int page = (int)blockIdx.x * kStretch + threadIdx.x * kPerThread + __ffs(m) - 1;
-    int lo = 0, hi = p.batch;  // first row whose ranks start past this one
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if ((local ? first_lds[mid] : w.first[mid]) <= rank) lo = mid + 1;
-      else hi = mid;
-    }
-    const int b = lo - 1;
-    p.table[(int64_t)b * p.max_pages + w.have[b] + rank - (local ? first_lds[b] : w.first[b])] = page;
-    p.refs[page] = 1;
-  }
+  take_stretch(p, w, blockIdx.x, base, limit, tmp, first_lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -410,35 +429,15 @@ __global__ __launch_bounds__(kBlock) void k_pages_copy(Pools pools, int64_t n_pa
 // ---------------------------------------------------------------------------
 // compact
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(kPlan) void k_compact_plan(PagesParams p, PageWork w, int32_t *n_live) {
-  __shared__ int tmp[kPlan / 64];
-  if (!count_stretch<true>(p, w, tmp)) return;
-  const int n = plan_bases(w, tmp);
-  // Live pages below n: those of the stretches before n's, and of its own.
-  __syncthreads();
-  const int s = n / kStretch;
-  int c = 0;
-  for (int64_t i = (int64_t)s * kStretch + threadIdx.x; i < n; i += kPlan) c += p.refs[i] > 0;
+// Movers and holes of stretch s in ascending order, `before` live pages before
+// it; a mover's entry of remap holds its rank i as -2 - i until k_compact_move has
+// put the page there.
+__device__ __forceinline__ void list_stretch(const PagesParams &p, const PageWork &w, int s, int before,
+                                             int n, int below, int32_t *remap, int *tmp) {
+  const uint32_t mine = stretch_bits<true>(p, s);
   int total;
-  block_excl_scan<kPlan>(c, tmp, &total);
-  if (threadIdx.x == 0) {
-    const int64_t last = (p.n_pages + kStretch - 1) / kStretch;
-    const int below = (s < last ? w.base[s] : n) + total;
-    w.scalar[kLive] = n;
-    w.scalar[kMoves] = n - below;
-    *n_live = n;
-  }
-}
-
-// Movers and holes in ascending order; a mover's entry of remap holds its rank
-// i as -2 - i until k_compact_move has put the page there.
-__global__ __launch_bounds__(kPlan) void k_compact_lists(PagesParams p, PageWork w, int32_t *remap) {
-  __shared__ int tmp[kPlan / 64];
-  const int n = w.scalar[kLive], below = n - w.scalar[kMoves];
-  const uint32_t mine = stretch_bits<true>(p, blockIdx.x);
-  int total;
-  int live = w.base[blockIdx.x] + block_excl_scan<kPlan>(__popc(mine), tmp, &total);
-  const int64_t p0 = (int64_t)blockIdx.x * kStretch + threadIdx.x * kPerThread;
+  int live = before + block_excl_scan<kPlan>(__popc(mine), tmp, &total);
+  const int64_t p0 = (int64_t)s * kStretch + threadIdx.x * kPerThread;
   for (int i = 0; i < kPerThread; ++i) {
     const int64_t page = p0 + i;
     if (page >= p.n_pages) return;
@@ -455,6 +454,35 @@ __global__ __launch_bounds__(kPlan) void k_compact_lists(PagesParams p, PageWork
       if (page < n) w.hole[page - live] = (int)page;
     }
   }
+}
+
+__global__ __launch_bounds__(kPlan) void k_compact_plan(PagesParams p, PageWork w, int32_t *remap,
+                                                        int32_t *n_live) {
+  __shared__ int tmp[kPlan / 64];
+  if (!count_stretch<true>(p, w, tmp)) return;
+  const int n = plan_bases(w, tmp);
+  // Live pages below n: those of the stretches before n's, and of its own.
+  __syncthreads();
+  const int s = n / kStretch;
+  int c = 0;
+  for (int64_t i = (int64_t)s * kStretch + threadIdx.x; i < n; i += kPlan) c += p.refs[i] > 0;
+  int total;
+  block_excl_scan<kPlan>(c, tmp, &total);
+  const int64_t last = (p.n_pages + kStretch - 1) / kStretch;
+  const int below = (s < last ? w.base[s] : n) + total;
+  if (threadIdx.x == 0) {
+    w.scalar[kLive] = n;
+    w.scalar[kMoves] = n - below;
+    *n_live = n;
+  }
+  if (p.n_pages <= kOneLaunch)
+    for (int i = 0; i < (int)gridDim.x; ++i) list_stretch(p, w, i, w.base[i], n, below, remap, tmp);
+}
+
+__global__ __launch_bounds__(kPlan) void k_compact_lists(PagesParams p, PageWork w, int32_t *remap) {
+  __shared__ int tmp[kPlan / 64];
+  const int n = w.scalar[kLive];
+  list_stretch(p, w, blockIdx.x, w.base[blockIdx.x], n, n - w.scalar[kMoves], remap, tmp);
 }
 
 // The table first (workgroups [0, batch)): an entry reads its page's rank or,
@@ -501,7 +529,7 @@ hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_
   PageWork w;
   carve_pages(p.n_pages, p.batch, work, &w);
   k_extend_plan<<<counters(p.n_pages), kPlan, 0, st>>>(p, w, grow, status);
-  k_extend_take<<<counters(p.n_pages), kPlan, 0, st>>>(p, w);
+  if (p.n_pages > kOneLaunch) k_extend_take<<<counters(p.n_pages), kPlan, 0, st>>>(p, w);
   return hipGetLastError();
 }
 
@@ -539,8 +567,8 @@ hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_
   carve_pages(p.n_pages, p.batch, work, &w);
   const unsigned n = counters(p.n_pages);
   const int pieces = pieces_of(pools);
-  k_compact_plan<<<n, kPlan, 0, st>>>(p, w, n_live);
-  k_compact_lists<<<n, kPlan, 0, st>>>(p, w, remap);
+  k_compact_plan<<<n, kPlan, 0, st>>>(p, w, remap, n_live);
+  if (p.n_pages > kOneLaunch) k_compact_lists<<<n, kPlan, 0, st>>>(p, w, remap);
   const int writers = (int)(n < 64 ? n : 64);
   const int64_t movers = std::min<int64_t>((int64_t)p.n_pages / 2 * pieces, 2048);
   k_compact_move<<<(unsigned)(p.batch + writers + movers), kBlock, 0, st>>>(p, w, pools, remap,

@@ -224,3 +224,36 @@ def test_captured_beam_steps(sd):
         model_pair(parents, g)
         same(m, a, pools)
         assert (b.block_table == -1).all() and (b.seq_lens == 0).all()
+
+
+@pytest.mark.parametrize("rows,width,pages", [(40, 300, 8191), (40, 300, 8192), (40, 300, 8193),
+                                              (40, 200, 2048), (40, 200, 4097), (5000, 3, 6000),
+                                              (5000, 3, 9000)])
+def test_pools_and_rows_around_what_one_workgroup_holds(sd, rows, width, pages):
+    # (pools that the planning workgroup hands out itself, and larger ones; rows
+    # that fit its LDS, and more)
+    rng = np.random.default_rng(pages + rows)
+    m, p, _ = model_and_pages(sd, random_state(rng, rows, width, pages), [])
+    for step in range(2):
+        grow = rng.integers(-3, 16 * width // 2 + 2, rows)
+        status = sd.sparse_decode_pages_extend(p, cuda(grow))
+        assert np.array_equal(status.cpu().numpy(), m.extend(grow))
+        same(m, p)
+        gone = rng.integers(-2, rows + 2, rows // 3)
+        sd.sparse_decode_pages_free(p, cuda(gone))
+        m.free(gone)
+        same(m, p)
+    remap, live = sd.sparse_decode_pages_compact(p)
+    want, n = m.compact()
+    assert int(live) == n and np.array_equal(remap.cpu().numpy(), want)
+    same(m, p)
+    n = rows + 7
+    parents = rng.integers(-1, rows + 1, n)
+    to = sd.Pages(torch.full((n, width), -1, dtype=torch.int32, device="cuda"),
+                  torch.zeros(n, dtype=torch.int32, device="cuda"), p.refs)
+    status = sd.sparse_decode_pages_fork(p, to, cuda(parents), keep=False)
+    table, lens, want = m.fork(n, parents, False)
+    assert np.array_equal(status.cpu().numpy(), want)
+    assert np.array_equal(to.block_table.cpu().numpy(), table)
+    assert np.array_equal(to.seq_lens.cpu().numpy(), lens)
+    same(m, p)
