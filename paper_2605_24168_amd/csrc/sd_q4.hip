@@ -2,7 +2,7 @@
 //
 // Both are bound by memory: 256 bytes (bfloat16) on one side of a row, 68 on
 // the other, and some 10 operations per channel pair.  250K positions of 8 KV
-// heads take 243 us to append and 270 to load: 5.4 and 4.8 TB/s of reads and
+// heads take 239 us to append and 266 to load: 5.5 and 5.0 TB/s of reads and
 // writes, where a copy reaches 4.8.  Sixteen lanes take a
 // row, eight channels each, so that a wave's loads and stores of four rows are
 // whole runs of 1 KB and 256 bytes.
