@@ -47,8 +47,8 @@ struct WindowParams {
 };
 
 // Workgroups of a call, from what the host knows: fills p.grid and what follows.
-// Partials take at most `scratch` bytes; part_bytes: those that they take (0: no
-// sequence is cut), and where they lie.
+// Partials take at most `scratch` bytes; *_part_bytes: those that they take (0: no
+// sequence is cut).
 void window_split(WindowParams &p, int kind, bool paged, size_t scratch);
 void chunk_split(WindowParams &p, int kind, size_t scratch);
 size_t token_part_bytes(const WindowParams &p);
