@@ -394,10 +394,11 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
 // bfloat16: the tiles go from memory straight into LDS, and a wave computes
 // the scores of one tile while it turns those of the tile before into weights,
 // so that the matrix unit and the vector unit have work at the same time.
-// 6618 tokens of 32 heads over windows of 4096: 479 us, 956 TFLOP/s of the 1243
-// that a large product reaches; the matrix unit is busy for 55% of the time that
-// a compute unit has work, the softmax's vector instructions for most of the
-// rest, and the last round of workgroups is a quarter full.
+// 6618 tokens of 32 heads over windows of 4096: 459-479 us, 956-997 TFLOP/s of
+// the 1243 that a large product reaches, with the last round of workgroups a
+// quarter full (1085 where it is full).  The matrix unit is busy for 55% of the
+// time that a compute unit has work, vector instructions for as long, at 1.9 GHz:
+// the clock falls under both (float32 runs at 2.4).
 // ---------------------------------------------------------------------------
 struct ChunkStage {
   u32x4 k[2][kChunkKeys * 16];   // tiles of keys and values, by parity
