@@ -396,7 +396,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
 // so that the matrix unit and the vector unit have work at the same time.
 // 6618 tokens of 32 heads over windows of 4096: 459-479 us, 956-997 TFLOP/s of
 // the 1243 that a large product reaches, with the last round of workgroups a
-// quarter full (1085 where it is full).  The matrix unit is busy for 55% of the
+// quarter full (8192 tokens over windows of 16384: 1063).  The matrix unit is busy for 55% of the
 // time that a compute unit has work, vector instructions for as long, at 1.9 GHz:
 // the clock falls under both (float32 runs at 2.4).
 // ---------------------------------------------------------------------------
