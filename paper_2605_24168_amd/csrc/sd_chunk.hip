@@ -152,7 +152,10 @@ __device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, Chunk
   const int y = (int)(blockIdx.x / (uint32_t)p.hkv);
   it.s = 0;
   it.n = 1;
-  if (p.plans == 0) return chunk_item<ROWS>(p, y, it);
+  // (The last row tiles first: without a window they see the most, and what ends
+  // a launch should be short: 8192 tokens over themselves 575 -> 535 us, 4096
+  // 169 -> 154, float32 2048 316 -> 289.)
+  if (p.plans == 0) return chunk_item<ROWS>(p, (int)(gridDim.x / (uint32_t)p.hkv) - 1 - y, it);
   auto queries = [&](int b, int &start) {
     start = (int)clamp_start(p.q_starts, b, p.n_rows);
     return max(0, (int)clamp_start(p.q_starts, b + 1, p.n_rows) - start);
