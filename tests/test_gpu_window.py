@@ -363,3 +363,31 @@ def test_empty_calls(sd):
     none = torch.zeros(2, dtype=torch.int32, device="cuda")
     out = sd.sparse_decode_window_attention(q, pr.cache, pr.dev_lens, sd.Window(), q_starts=none)
     assert out.shape == (0, 4, 128)
+
+
+def test_two_graphs_replayed_in_turn(sd):
+    # (both keep partials in the library's memory; one stream orders them)
+    a = Problem(sd, [5000, 40, 1200], 8, 2, "paged", "bf16", seed=31)
+    b = Problem(sd, [4000, 700], 8, 2, "bhnd", "bf16", counts=[6, 2], seed=32)
+    calls = []
+    for pr, packed in ((a, False), (b, True)):
+        q, starts = pr.q.cuda(), pr.starts.cuda() if packed else None
+        out = torch.zeros_like(q)
+        run = lambda pr=pr, q=q, starts=starts, out=None: sd.sparse_decode_window_attention(
+            q, pr.cache, pr.dev_lens, sd.Window(8, 4500), q_starts=starts, out=out)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run(out=out)
+        calls.append((run, graph, out))
+    for step in range(4):
+        for _, graph, out in calls:
+            out.zero_()
+            graph.replay()
+        calls[step % 2][0]()          # an eager call between the replays
+        for run, graph, out in calls:
+            graph.replay()
+        torch.cuda.synchronize()
+        for run, _, out in calls:
+            assert torch.equal(out, run())
+        a.dev_lens -= 3
+        b.dev_lens -= 1
