@@ -79,10 +79,11 @@ struct QRegs {
 };
 
 // Query operand: lane (head, quarter a) supplies the channels that the key
-// operand of the same instruction and quarter holds.
-template <int KIND>
+// operand of the same instruction and quarter holds.  TWICE: heads are 0..7, and
+// again on the lanes from 8 on.
+template <int KIND, bool TWICE>
 __device__ __forceinline__ void load_query(const WindowParams &p, int b, int g, QRegs<KIND> &qr) {
-  const int l = lane_id(), h = l & 15, a = l >> 4;
+  const int l = lane_id(), h = l & (TWICE ? 7 : 15), a = l >> 4;
   constexpr int n = KIND == kCacheF32 ? 8 : 4;
 #pragma unroll
   for (int i = 0; i < n; ++i) qr.v[i] = u32x4{0u, 0u, 0u, 0u};
@@ -174,7 +175,10 @@ __device__ __forceinline__ void q4_values(uint32_t codes, float scale, uint32_t 
   out[3] = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
 }
 
-__device__ __forceinline__ bf16x8 as_bf16(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
+__device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
+                                                 __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+}
 
 template <int KIND>
 __device__ __forceinline__ f32x4 tile_scores(const QRegs<KIND> &q, const Tile<KIND> &t) {
@@ -190,15 +194,14 @@ __device__ __forceinline__ f32x4 tile_scores(const QRegs<KIND> &q, const Tile<KI
   } else if constexpr (KIND == kCacheBf16) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(t.k[i]), as_bf16(q.v[i]), s, 0, 0, 0);
+      s = mfma16(t.k[i], q.v[i], s);
   } else {
     const float scale = __uint_as_float(t.ks << 23);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t w[4];
       q4_values(t.k[i], scale, w);
-      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(u32x4{w[0], w[1], w[2], w[3]}),
-                                                  as_bf16(q.v[i]), s, 0, 0, 0);
+      s = mfma16(u32x4{w[0], w[1], w[2], w[3]}, q.v[i], s);
     }
   }
   return s;
@@ -228,7 +231,7 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) {
 // O^T += V^T p^T over two tiles.  acc[e] holds, in lane (head, quarter a),
 // register r: channel 32 a + 8 r + e (bfloat16 and 4 bits; e = 0..7), or
 // 64 (e / 4) + 16 a + 4 r + e % 4 (float32).
-template <int KIND>
+template <int KIND, bool TWICE>
 __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, const Tile<KIND> &tb,
                                            const float pa[4], const float pb[4]) {
   if constexpr (KIND == kCacheF32) {
@@ -241,11 +244,28 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
         acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(y), pb[r], acc[e], 0, 0, 0);
       }
   } else {
-    // The weights are rounded to bfloat16 (half a step, 2^-9 relative), as
-    // the values are: the rounding errors of a row's weights are independent
-    // and the output's own rounding is as large.
-    const bf16x8 w = as_bf16(u32x4{pack2(pa[0], pa[1]), pack2(pa[2], pa[3]),
-                                   pack2(pb[0], pb[1]), pack2(pb[2], pb[3])});
+    // Two bfloat16 numbers hold a weight, its upper half and what that leaves, so
+    // that of the output only its own rounding remains: together they are off by
+    // 2^-15 of the weight at most.  (One is off by 2^-8, as much as the output's own
+    // rounding, and all weights of a row may be off to one side.)  The matrix unit
+    // has the time: 64 sequences of bfloat16 171 us with one and with two.  In 4 bits, where the vector unit is busy too,
+    // lanes from 8 on hold the second number of the heads below (TWICE) instead of
+    // an instruction of its own, and both are cut off (2^-14): 16 of 128K take 366
+    // us, with rounding 372, with instructions 375, and 357 with one number.
+    u32x4 w, rest;
+    const uint32_t mask = !TWICE || (lane_id() & 8) ? 0xFFFF0000u : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float y0 = i < 2 ? pa[2 * i] : pb[2 * i - 4], y1 = i < 2 ? pa[2 * i + 1] : pb[2 * i - 3];
+      const float r0 = y0 - __uint_as_float(__float_as_uint(y0) & mask);
+      const float r1 = y1 - __uint_as_float(__float_as_uint(y1) & mask);
+      if constexpr (TWICE) {
+        w[i] = high_halves(__float_as_uint(r0), __float_as_uint(r1));
+      } else {
+        w[i] = high_halves(__float_as_uint(y0), __float_as_uint(y1));
+        rest[i] = pack2(r0, r1);
+      }
+    }
     uint32_t x[8][4];  // channel pairs 2d, 2d + 1 of this lane's 8 rows
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -272,8 +292,12 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
         lo[i] = low_halves(x[2 * i][d], x[2 * i + 1][d]);
         hi[i] = high_halves(x[2 * i][d], x[2 * i + 1][d]);
       }
-      acc[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(lo), w, acc[2 * d], 0, 0, 0);
-      acc[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(hi), w, acc[2 * d + 1], 0, 0, 0);
+      acc[2 * d] = mfma16(lo, w, acc[2 * d]);
+      acc[2 * d + 1] = mfma16(hi, w, acc[2 * d + 1]);
+      if constexpr (!TWICE) {
+        acc[2 * d] = mfma16(lo, rest, acc[2 * d]);
+        acc[2 * d + 1] = mfma16(hi, rest, acc[2 * d + 1]);
+      }
     }
   }
 }
@@ -301,7 +325,7 @@ static constexpr int part_cost(int kind) { return kind == kCacheQ4 ? 50 : 13; }
 // same time, then slots.  HEADS: KV heads of a workgroup, each with NW / HEADS
 // waves.  The waves of a workgroup take the steps of two tiles in turn, each
 // with the loads of its next step under way while it computes.
-template <int KIND, bool PAGED, int NW, int HEADS>
+template <int KIND, bool PAGED, int NW, int HEADS, bool TWICE>
 __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_attend(WindowParams p) {
   constexpr int NS = NW / HEADS;   // waves of a head
   extern __shared__ float lds[];
@@ -339,7 +363,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   const int t0 = part.s * part.span * kStep, t1 = min(tr.n, t0 + part.span * kStep);
 
   QRegs<KIND> qr;
-  load_query<KIND>(p, b, g, qr);
+  load_query<KIND, TWICE>(p, b, g, qr);
   const Offsets<KIND> offs(kInside ? p.hkv : 1);
 
   float m = kFloor, ls = 0.f;  // of this lane's head; ls over its own positions
@@ -435,7 +459,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
         pw[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], p.scale2, -m));
         ls += pw[u][r];
       }
-    add_values<KIND>(acc, st.tile[0], st.tile[1], pw[0], pw[1]);
+    add_values<KIND, TWICE>(acc, st.tile[0], st.tile[1], pw[0], pw[1]);
   };
 
   // (Loads past the last step touch no memory, and being unconditional let the
@@ -460,6 +484,12 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   ls += __shfl_xor(ls, 16);
   ls += __shfl_xor(ls, 32);
   const int h = l & 15;
+  if constexpr (TWICE) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[e][r] += __shfl_xor(acc[e][r], 8);
+  }
   float *ml = lds, *o = lds + 2 * NW * p.G;
   constexpr int kRow = kHeadDim + 4;  // heads start 4 banks apart
   if (h < p.G) {
@@ -581,11 +611,11 @@ size_t token_part_bytes(const WindowParams &p) {
   return (size_t)p.grid * p.G * (p.quad ? 4 : 1) * kPartStride * sizeof(float);
 }
 
-template <int KIND, bool PAGED, int HEADS>
+template <int KIND, bool PAGED, int HEADS, bool TWICE = false>
 static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
   constexpr int NW = token_waves(KIND);
   if (p.grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_token_attend<KIND, PAGED, NW, HEADS>
+  k_token_attend<KIND, PAGED, NW, HEADS, TWICE>
       <<<(unsigned)p.grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
   return hipGetLastError();
 }
@@ -595,8 +625,10 @@ hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipS
   switch (kind) {
     case kCacheF32: return paged ? launch_token<kCacheF32, true, 1>(p, st) : launch_token<kCacheF32, false, 1>(p, st);
     case kCacheBf16: return paged ? launch_token<kCacheBf16, true, 1>(p, st) : launch_token<kCacheBf16, false, 1>(p, st);
-    default: return paged ? launch_token<kCacheQ4, true, 1>(p, st) : launch_token<kCacheQ4, false, 1>(p, st);
   }
+  if (p.G <= 8)
+    return paged ? launch_token<kCacheQ4, true, 1, true>(p, st) : launch_token<kCacheQ4, false, 1, true>(p, st);
+  return paged ? launch_token<kCacheQ4, true, 1>(p, st) : launch_token<kCacheQ4, false, 1>(p, st);
 }
 
 }  // namespace sd
