@@ -381,6 +381,11 @@ typedef struct {
  * queries of the call undefined.  Positions on pages outside the pool (a block
  * table entry below 0 or past its last page) are seen by no query.  Scores are
  * at most 2^28 in magnitude (rounding them to 32 bits would move weights).
+ * Sums and statistics are float32.  The weights of bfloat16 calls are rounded to
+ * bfloat16 where q_starts is given, and kept to 2^-14 of themselves where it is
+ * not; out is a weighted mean of the values in either case.  (One query that sees
+ * everything is what sparse_decode_dense_attention computes, whose weights are
+ * float32 and which takes up to 8 query heads for a KV head.)
  */
 sd_status sparse_decode_window_attention(const sd_tensor *q, const sd_kv *K, const sd_kv *V,
                                          const int32_t *seq_lens, const int32_t *q_starts,

@@ -248,10 +248,11 @@ __device__ __forceinline__ void add_values(f32x4 acc[8], const Tile<KIND> &ta, c
     // that of the output only its own rounding remains: together they are off by
     // 2^-15 of the weight at most.  (One is off by 2^-8, as much as the output's own
     // rounding, and all weights of a row may be off to one side.)  The matrix unit
-    // has the time: 64 sequences of bfloat16 171 us with one and with two.  In 4 bits, where the vector unit is busy too,
-    // lanes from 8 on hold the second number of the heads below (TWICE) instead of
-    // an instruction of its own, and both are cut off (2^-14): 16 of 128K take 366
-    // us, with rounding 372, with instructions 375, and 357 with one number.
+    // has the time: 64 sequences of bfloat16 171 us with one and with two.  In 4
+    // bits, where the vector unit is busy too, lanes from 8 on hold the second number
+    // of the heads below (TWICE) instead of an instruction of its own, and both are
+    // cut off (2^-14): 16 of 128K take 366 us, with rounding 372, with instructions
+    // 375, and 357 with one number.
     u32x4 w, rest;
     const uint32_t mask = !TWICE || (lane_id() & 8) ? 0xFFFF0000u : 0u;
 #pragma unroll

@@ -118,3 +118,21 @@ def test_one_query_rounds_its_output_only(sd, L, hq, hkv):
     out = sd.sparse_decode_q4_attention(q.cuda(), c, lens)
     ref, allow = one_query_bound(q, R.q4_round(k)[0], R.q4_round(v)[0], scale)
     assert ((out.double().cpu() - ref).abs() <= allow).all()
+
+
+@pytest.mark.parametrize("layout", ["bhnd", "paged"])
+@pytest.mark.parametrize("L,n", [(2, 2), (40, 9), (64, 64), (200, 3), (2399, 130)])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (16, 1), (3, 3)])
+def test_a_mean_of_equal_values_is_that_value_for_every_query(sd, layout, L, n, hq, hkv):
+    k, v, value = equal_values(2, hkv, L, L)
+    table = None
+    if layout == "paged":
+        (k, table), (v, _) = paged(k), paged(v)
+    cache = sd.KVCache(k=k, v=v, layout=layout, block_table=table)
+    lens = torch.full((2,), L, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, n, n + 1], dtype=torch.int32, device="cuda")
+    q = torch.zeros((n + 1, hq, 128), dtype=torch.bfloat16, device="cuda")
+    q[..., :2] = 1
+    want = value[:, :, 0].repeat_interleave(hq // hkv, 1).cuda()
+    out = sd.sparse_decode_window_attention(q, cache, lens, sd.Window(softmax_scale=LN2), q_starts=starts)
+    assert torch.equal(out, torch.cat((want[:1].expand(n, -1, -1), want[1:])))
