@@ -322,7 +322,9 @@ sd_status sparse_decode_profile_mean(sd_profile *out, int32_t *n_calls);
  * cost rule (rows expecting 8K candidates or more); flags & 64, and 16 and
  * 32 too, keep calls on the candidate path whose rows the cost rule for
  * short contexts would select from their full scores (it goes by the cache's
- * capacity: the sequences' lengths are device memory).  0 restores normal. */
+ * capacity: the sequences' lengths are device memory); with flags & 128,
+ * window attention, 4-bit attention and page calls find in their workgroups'
+ * counters what a call before them left unfinished.  0 restores normal. */
 sd_status sparse_decode_set_debug(int32_t flags);
 
 /* Measurement helper, not a step of the method: one streaming read of

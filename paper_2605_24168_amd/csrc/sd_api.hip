@@ -55,6 +55,7 @@ std::mutex g_mu;
 DevState g_dev[kMaxDevices];
 std::atomic<int> g_profiling{0};
 std::atomic<int> g_debug{0};
+uint64_t g_counted = 0;   // calls that count workgroups (with g_mu held)
 
 struct Shape {
   int B, Hq, Hkv, G, R;
@@ -1271,6 +1272,14 @@ char *static_scratch(size_t bytes, sd_status &st) {
   return st ? nullptr : (char *)ds->scratch;
 }
 
+// The next call whose workgroups count themselves.  (Called with g_mu held.)
+sd::Counting next_count(void *stream) {
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  const bool captured =
+      hipStreamIsCapturing((hipStream_t)stream, &cs) == hipSuccess && cs != hipStreamCaptureStatusNone;
+  return sd::Counting{++g_counted, captured, (g_debug.load() & 128) != 0};
+}
+
 // Splits, scratch and launches of a call.
 sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
   const bool packed = p.q_starts != nullptr;
@@ -1285,7 +1294,8 @@ sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
     if (packed) p.part_n = (int32_t *)(p.part + p.n_rows * p.hq * p.nsplit * sd::kPartStride);
   }
   return hip_status(packed ? sd::launch_chunk_attend(p, kind, paged, (hipStream_t)stream)
-                           : sd::launch_token_attend(p, kind, paged, (hipStream_t)stream));
+                           : sd::launch_token_attend(p, kind, paged, next_count(stream),
+                                                     (hipStream_t)stream));
 }
 
 }  // namespace
@@ -1472,13 +1482,13 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   return na && nb && x < y + nb && y < x + na;
 }
 
-// The scratch of the page calls, as f(base).
+// The scratch of the page calls and their count, as f(base, count).
 template <class F>
-sd_status with_pages_work(int64_t n_pages, int64_t batch, F f) {
+sd_status with_pages_work(int64_t n_pages, int64_t batch, void *stream, F f) {
   std::lock_guard<std::mutex> lk(g_mu);
   sd_status st = SD_OK;
   char *base = static_scratch(sd::pages_work_bytes(n_pages, batch), st);
-  return st ? st : hip_status(f(base));
+  return st ? st : hip_status(f(base, next_count(stream)));
 }
 
 }  // namespace
@@ -1491,8 +1501,9 @@ sd_status sparse_decode_pages_extend(const sd_pages *pages, const int32_t *grow,
   if (st) return st;
   if (pages->batch == 0) return SD_OK;
   if (!grow || !status) return SD_ERR_INVALID_ARG;
-  return with_pages_work(pages->n_pages, pages->batch, [&](char *base) {
-    return sd::launch_pages_extend(pages_params(pages), grow, status, base, (hipStream_t)stream);
+  return with_pages_work(pages->n_pages, pages->batch, stream, [&](char *base, const sd::Counting &c) {
+    return sd::launch_pages_extend(pages_params(pages), grow, status, base, c,
+                                   (hipStream_t)stream);
   });
 }
 
@@ -1515,9 +1526,10 @@ sd_status sparse_decode_pages_fork(const sd_pages *from, const sd_pages *to,
   if (st) return st;
   if (from->batch == 0 && to->batch == 0) return SD_OK;
   if (to->batch > 0 && (!parents || !status)) return SD_ERR_INVALID_ARG;
-  return with_pages_work(n_pages, std::max(from->batch, to->batch), [&](char *base) {
+  return with_pages_work(n_pages, std::max(from->batch, to->batch), stream,
+                         [&](char *base, const sd::Counting &c) {
     return sd::launch_pages_fork(pages_params(from), pages_params(to), parents, keep != 0, pl,
-                                 status, base, (hipStream_t)stream);
+                                 status, base, c, (hipStream_t)stream);
   });
 }
 
@@ -1555,8 +1567,8 @@ sd_status sparse_decode_pages_compact(const sd_pages *pages, const sd_tensor *po
   st = check_pools(pools, n_pools, n_pages, pl);
   if (st) return st;
   if (!n_live || (n_pages > 0 && !remap)) return SD_ERR_INVALID_ARG;
-  return with_pages_work(n_pages, pages->batch, [&](char *base) {
-    return sd::launch_pages_compact(pages_params(pages), pl, remap, n_live, base,
+  return with_pages_work(n_pages, pages->batch, stream, [&](char *base, const sd::Counting &c) {
+    return sd::launch_pages_compact(pages_params(pages), pl, remap, n_live, base, c,
                                     (hipStream_t)stream);
   });
 }

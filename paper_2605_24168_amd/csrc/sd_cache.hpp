@@ -44,7 +44,20 @@ struct WindowParams {
   int32_t rounds[3];           // of workgroups on all compute units, for each of them
   int32_t slots[3];            // their workgroups for each group of KV heads
   int32_t part_cost;           // of a workgroup beside its units, in sixteenths of one
+  uint64_t call;               // see Counting
 };
+
+// How the workgroups of a launch find out which of them is the last.  A counter's
+// upper bits name the call that counts in it, and calls have ascending numbers, so
+// that whatever another call left there counts for nothing, calls that overlapped
+// against the rules included.  A captured call comes with its number again and
+// again: it sets its counters by a launch of their own.
+struct Counting {
+  uint64_t call;
+  bool captured;
+  bool spoil;    // (for tests) finds what a call before it left unfinished
+};
+constexpr int kCountBits = 20;   // more than the workgroups that share a counter
 
 // Workgroups of a call, from what the host knows: fills p.grid and what follows.
 // Partials take at most `scratch` bytes; *_part_bytes: those that they take (0: no
@@ -53,7 +66,7 @@ void window_split(WindowParams &p, int kind, bool paged, size_t scratch);
 void chunk_split(WindowParams &p, int kind, size_t scratch);
 size_t token_part_bytes(const WindowParams &p);
 size_t chunk_part_bytes(const WindowParams &p);
-hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
+hipError_t launch_token_attend(WindowParams p, int kind, bool paged, const Counting &c, hipStream_t st);
 hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
 
 // Writing and reading a 4-bit cache.
@@ -83,15 +96,15 @@ struct PagesParams {
 };
 size_t pages_work_bytes(int64_t n_pages, int64_t batch);
 hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_t *status,
-                               char *work, hipStream_t st);
+                               char *work, const Counting &c, hipStream_t st);
 hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
                              const int32_t *parents, bool keep, const Pools &pools,
-                             int32_t *status, char *work, hipStream_t st);
+                             int32_t *status, char *work, const Counting &c, hipStream_t st);
 hipError_t launch_pages_free(const PagesParams &p, const int32_t *rows, int64_t n, hipStream_t st);
 hipError_t launch_pages_copy(const Pools &pools, int64_t n_pages, const int32_t *src,
                              const int32_t *dst, int64_t n, hipStream_t st);
 hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_t *remap,
-                                int32_t *n_live, char *work, hipStream_t st);
+                                int32_t *n_live, char *work, const Counting &c, hipStream_t st);
 
 // Two floats rounded to bfloat16 (to nearest even), the first in the low half.
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -110,6 +123,15 @@ struct Joined {
 // past the caches that are not common to both.
 __device__ __forceinline__ void put_shared(float *at, float x) {
   __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// One thread of each of the n workgroups that share a counter: call_counter, then
+// (with what it is to hand on stored and waited for) counted_last.
+__device__ __forceinline__ void call_counter(uint64_t *at, uint64_t call) {
+  __hip_atomic_fetch_max(at, call << kCountBits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool counted_last(uint64_t *at, uint32_t n) {
+  const uint64_t before = __hip_atomic_fetch_add(at, (uint64_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return ((uint32_t)before & ((1u << kCountBits) - 1)) == n - 1;
 }
 template <bool SHARED>
 __device__ __forceinline__ float get_partial(const float *at) {

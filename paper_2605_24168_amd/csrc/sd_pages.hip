@@ -44,6 +44,7 @@ struct PageWork {
   int32_t *list;      // [pages / 2]: compact: movers; fork: a child's own last page
   int32_t *hole;      // [pages / 2]: compact: holes; fork: [0, batch) a child's rank among those
                       // that get a page, [batch, ..) the page that it copies
+  uint64_t call;      // see Counting
 };
 enum { kLimit = 0, kMoves = 1, kLive = 2 };
 
@@ -94,24 +95,27 @@ __device__ __forceinline__ uint32_t stretch_bits(const PagesParams &p, int s) {
   return m;
 }
 
-// Workgroups of the counting launch that are done; 0 between calls.
-static __device__ uint32_t stretches_done;
+// Workgroups of the counting launch that are done.
+static __device__ uint64_t stretches_done;
+
+__global__ void k_pages_counter(uint64_t x) { stretches_done = x; }
 
 // Counts this workgroup's stretch; true for the workgroup that counts last,
 // which finds all counts in w.base.  (They are stored past the caches that
 // workgroups do not share, and have arrived before a workgroup counts itself.)
 template <bool LIVE>
 __device__ __forceinline__ bool count_stretch(const PagesParams &p, const PageWork &w, int *tmp) {
-  __shared__ uint32_t before;
+  __shared__ bool last;
   int total;
   block_excl_scan<kPlan>(__popc(stretch_bits<LIVE>(p, blockIdx.x)), tmp, &total);
   if (threadIdx.x == 0) {
+    call_counter(&stretches_done, w.call);
     __hip_atomic_store(&w.base[blockIdx.x], total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    before = atomicInc(&stretches_done, gridDim.x - 1);
+    last = counted_last(&stretches_done, gridDim.x);
   }
   __syncthreads();
-  return before == gridDim.x - 1;
+  return last;
 }
 
 // Counts of the launch's stretches to the pages before each; returns all of
@@ -521,13 +525,20 @@ __global__ __launch_bounds__(kBlock) void k_compact_move(PagesParams p, PageWork
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
+static void start_count(PageWork &w, const Counting &c, hipStream_t st) {
+  w.call = c.call;
+  if (c.spoil) k_pages_counter<<<1, 1, 0, st>>>(((c.call - 1) << kCountBits) + 1);
+  if (c.captured) k_pages_counter<<<1, 1, 0, st>>>(c.call << kCountBits);
+}
+
 // Workgroups of a counting launch (one at least: it also plans).
 static unsigned counters(int64_t n_pages) { return (unsigned)std::max<int64_t>(stretches(n_pages), 1); }
 
 hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_t *status,
-                               char *work, hipStream_t st) {
+                               char *work, const Counting &c, hipStream_t st) {
   PageWork w;
   carve_pages(p.n_pages, p.batch, work, &w);
+  start_count(w, c, st);
   k_extend_plan<<<counters(p.n_pages), kPlan, 0, st>>>(p, w, grow, status);
   if (p.n_pages > kOneLaunch) k_extend_take<<<counters(p.n_pages), kPlan, 0, st>>>(p, w);
   return hipGetLastError();
@@ -535,12 +546,13 @@ hipError_t launch_pages_extend(const PagesParams &p, const int32_t *grow, int32_
 
 hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
                              const int32_t *parents, bool keep, const Pools &pools,
-                             int32_t *status, char *work, hipStream_t st) {
+                             int32_t *status, char *work, const Counting &c, hipStream_t st) {
   PageWork w;
   carve_pages(from.n_pages, from.batch > to.batch ? from.batch : to.batch, work, &w);
   const int pieces = pieces_of(pools);
   const int64_t last = from.batch + (int64_t)to.batch * (pieces + 1);
   if (last > INT32_MAX) return hipErrorInvalidConfiguration;
+  start_count(w, c, st);
   k_fork_plan<<<counters(from.n_pages), kPlan, 0, st>>>(from, to, w, parents, keep ? 1 : 0, status);
   if (to.batch) k_fork_rows<<<(unsigned)to.batch, kBlock, 0, st>>>(from, to, w);
   k_fork_pages<<<(unsigned)last, kBlock, 0, st>>>(from, to, w, pools, pieces, keep ? 1 : 0);
@@ -562,9 +574,10 @@ hipError_t launch_pages_copy(const Pools &pools, int64_t n_pages, const int32_t 
 }
 
 hipError_t launch_pages_compact(const PagesParams &p, const Pools &pools, int32_t *remap,
-                                int32_t *n_live, char *work, hipStream_t st) {
+                                int32_t *n_live, char *work, const Counting &c, hipStream_t st) {
   PageWork w;
   carve_pages(p.n_pages, p.batch, work, &w);
+  start_count(w, c, st);
   const unsigned n = counters(p.n_pages);
   const int pieces = pieces_of(pools);
   k_compact_plan<<<n, kPlan, 0, st>>>(p, w, remap, n_live);

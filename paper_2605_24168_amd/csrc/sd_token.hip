@@ -314,9 +314,13 @@ __device__ __forceinline__ void store_out(const WindowParams &p, int64_t at, flo
   else ((uint16_t *)p.out)[at] = f32_to_bf16_rne(x);
 }
 
-// Parts of a (sequence, group of KV heads) that are done; 0 between calls.
+// Parts of a (sequence, group of KV heads) that are done.
 constexpr int kSplitItems = 4096;
-static __device__ uint32_t splits_done[kSplitItems];
+static __device__ uint64_t splits_done[kSplitItems];
+
+__global__ __launch_bounds__(kBlock) void k_token_counters(int n, uint64_t x) {
+  for (int i = blockIdx.x * kBlock + threadIdx.x; i < n; i += gridDim.x * kBlock) splits_done[i] = x;
+}
 
 // What a workgroup costs beside its tiles, in sixteenths of a step of its waves
 // (131 KB of rows and 4.8 us, or 35 KB and 1.3 us in 4 bits; 4 us beside it).
@@ -481,6 +485,9 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     compute(i + 1, st[1]);
   }
 
+  uint64_t *const done = &splits_done[part.n > 1 ? b * groups + g0 / HEADS : 0];
+  if (part.n > 1 && threadIdx.x == 0) call_counter(done, p.call);
+
   // Join the waves: per head a common maximum, scaled sums and outputs.
   ls += __shfl_xor(ls, 16);
   ls += __shfl_xor(ls, 32);
@@ -539,14 +546,12 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   // The workgroup that finishes last joins the splits, a wave per query head.
   // Each one counts itself once its partials have arrived where every compute
   // unit sees them (which fences would ensure too, by writing back and
-  // emptying the L2 caches: 5 us more); the count wraps to 0 with the last,
-  // ready for the next call.
+  // emptying the L2 caches: 5 us more).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0)
-    *(uint32_t *)lds = atomicInc(&splits_done[b * groups + g0 / HEADS], (uint32_t)part.n - 1);
+  if (threadIdx.x == 0) *(uint32_t *)lds = counted_last(done, (uint32_t)part.n);
   __syncthreads();
-  if (*(volatile uint32_t *)lds != (uint32_t)part.n - 1) return;
+  if (!*(volatile uint32_t *)lds) return;
   const int64_t first = (int64_t)part.first * groups + g0 / HEADS;   // the item's workgroups
   for (int hh = w; hh < orows; hh += NW) {
     const Joined v = join_splits<true>(p.part + (first * orows + hh) * kPartStride,
@@ -621,7 +626,14 @@ static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_token_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
+hipError_t launch_token_attend(WindowParams p, int kind, bool paged, const Counting &c, hipStream_t st) {
+  p.call = c.call;
+  const int items = p.plans > 0 ? p.batch * (p.hkv / (p.quad ? 4 : 1)) : 0;
+  for (const bool left : {true, false}) {
+    if (items == 0 || !(left ? c.spoil : c.captured)) continue;
+    k_token_counters<<<(unsigned)((items + kBlock - 1) / kBlock), kBlock, 0, st>>>(
+        items, left ? ((c.call - 1) << kCountBits) + 1 : c.call << kCountBits);
+  }
   if (p.quad) return launch_token<kCacheBf16, true, 4>(p, st);
   switch (kind) {
     case kCacheF32: return paged ? launch_token<kCacheF32, true, 1>(p, st) : launch_token<kCacheF32, false, 1>(p, st);
