@@ -33,6 +33,9 @@ constexpr int kStretch = kPlan * kPerThread;      // pages counted by one workgr
 constexpr int kOneLaunch = 4 * kStretch;
 constexpr int64_t kPiece = 16 * 1024;             // bytes a workgroup copies at once
 constexpr int kMany = 1 << 29;                    // more than any number of pages
+// Workgroups of one launch, at most (a launch has less than 2^32 threads): where
+// there is more to do, each of them does several.
+constexpr int64_t kMostGroups = 1 << 23;
 
 // Scratch of one call (all int32).
 struct PageWork {
@@ -373,7 +376,8 @@ __device__ __forceinline__ void copy_piece(const Pools &pools, int64_t src, int6
 }
 
 // Workgroups [0, from.batch) count the pages of the parents' rows, and empty
-// those that the call ends; the others copy the part-filled pages.
+// those that the call ends; the others copy the part-filled pages, a piece of a
+// child's page each.
 __global__ __launch_bounds__(kBlock) void k_fork_pages(PagesParams from, PagesParams to, PageWork w,
                                                        Pools pools, int pieces, int keep) {
   int64_t i = blockIdx.x;
@@ -394,14 +398,16 @@ __global__ __launch_bounds__(kBlock) void k_fork_pages(PagesParams from, PagesPa
     }
     return;
   }
-  i -= from.batch;
-  const int child = (int)(i / (pieces + 1)), piece = (int)(i % (pieces + 1));
-  const int fresh = w.list[child], old = w.hole[to.batch + child];
-  if (fresh < 0) return;
-  if (piece == pieces) {
-    if (threadIdx.x == 0) from.refs[fresh] = 1;
-  } else if (in_pool(from, old)) {
-    copy_piece(pools, old, fresh, piece);
+  const int64_t groups = (int64_t)gridDim.x - from.batch;
+  for (i -= from.batch; i < (int64_t)to.batch * (pieces + 1); i += groups) {
+    const int child = (int)(i / (pieces + 1)), piece = (int)(i % (pieces + 1));
+    const int fresh = w.list[child], old = w.hole[to.batch + child];
+    if (fresh < 0) continue;
+    if (piece == pieces) {
+      if (threadIdx.x == 0) from.refs[fresh] = 1;
+    } else if (in_pool(from, old)) {
+      copy_piece(pools, old, fresh, piece);
+    }
   }
 }
 
@@ -410,24 +416,27 @@ __global__ __launch_bounds__(kBlock) void k_fork_pages(PagesParams from, PagesPa
 // ---------------------------------------------------------------------------
 // An entry is exchanged for -1, so that a row listed twice gives its pages
 // back once.
-__global__ __launch_bounds__(kBlock) void k_pages_free(PagesParams p, const int32_t *rows) {
-  const int b = rows[blockIdx.x];
-  if (b < 0 || b >= p.batch) return;
-  int32_t *row = p.table + (int64_t)b * p.max_pages;
-  for (int c = threadIdx.x; c < p.max_pages; c += kBlock) {
-    const int page = atomicExch(&row[c], -1);
-    if (in_pool(p, page)) atomicAdd(&p.refs[page], -1);
+__global__ __launch_bounds__(kBlock) void k_pages_free(PagesParams p, const int32_t *rows, int64_t n) {
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int b = rows[i];
+    if (b < 0 || b >= p.batch) continue;
+    int32_t *row = p.table + (int64_t)b * p.max_pages;
+    for (int c = threadIdx.x; c < p.max_pages; c += kBlock) {
+      const int page = atomicExch(&row[c], -1);
+      if (in_pool(p, page)) atomicAdd(&p.refs[page], -1);
+    }
+    if (threadIdx.x == 0) p.seq_lens[b] = 0;
   }
-  if (threadIdx.x == 0) p.seq_lens[b] = 0;
 }
 
 __global__ __launch_bounds__(kBlock) void k_pages_copy(Pools pools, int64_t n_pages,
                                                        const int32_t *src, const int32_t *dst,
-                                                       int pieces) {
-  const int64_t i = blockIdx.x / pieces;
-  const int64_t s = src[i], d = dst[i];
-  if (s < 0 || s >= n_pages || d < 0 || d >= n_pages || s == d) return;
-  copy_piece(pools, s, d, (int)(blockIdx.x % pieces));
+                                                       int64_t n, int pieces) {
+  for (int64_t i = blockIdx.x; i < n * pieces; i += gridDim.x) {
+    const int64_t s = src[i / pieces], d = dst[i / pieces];
+    if (s < 0 || s >= n_pages || d < 0 || d >= n_pages || s == d) continue;
+    copy_piece(pools, s, d, (int)(i % pieces));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -550,8 +559,7 @@ hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
   PageWork w;
   carve_pages(from.n_pages, from.batch > to.batch ? from.batch : to.batch, work, &w);
   const int pieces = pieces_of(pools);
-  const int64_t last = from.batch + (int64_t)to.batch * (pieces + 1);
-  if (last > INT32_MAX) return hipErrorInvalidConfiguration;
+  const int64_t last = from.batch + std::min((int64_t)to.batch * (pieces + 1), kMostGroups);
   start_count(w, c, st);
   k_fork_plan<<<counters(from.n_pages), kPlan, 0, st>>>(from, to, w, parents, keep ? 1 : 0, status);
   if (to.batch) k_fork_rows<<<(unsigned)to.batch, kBlock, 0, st>>>(from, to, w);
@@ -560,16 +568,15 @@ hipError_t launch_pages_fork(const PagesParams &from, const PagesParams &to,
 }
 
 hipError_t launch_pages_free(const PagesParams &p, const int32_t *rows, int64_t n, hipStream_t st) {
-  if (n > 0) k_pages_free<<<(unsigned)n, kBlock, 0, st>>>(p, rows);
+  if (n > 0) k_pages_free<<<(unsigned)std::min(n, kMostGroups), kBlock, 0, st>>>(p, rows, n);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_copy(const Pools &pools, int64_t n_pages, const int32_t *src,
                              const int32_t *dst, int64_t n, hipStream_t st) {
   const int pieces = pieces_of(pools);
-  const int64_t grid = n * pieces;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (grid > 0) k_pages_copy<<<(unsigned)grid, kBlock, 0, st>>>(pools, n_pages, src, dst, pieces);
+  const int64_t grid = std::min(n * pieces, kMostGroups);
+  if (grid > 0) k_pages_copy<<<(unsigned)grid, kBlock, 0, st>>>(pools, n_pages, src, dst, n, pieces);
   return hipGetLastError();
 }
 
