@@ -8,6 +8,10 @@
 
 namespace sd {
 
+// A launch has less than 2^32 threads: work for more workgroups than this is done in
+// several launches, or by several rounds of one's workgroups.
+constexpr int64_t kMostGroups = 1 << 22;
+
 // How a cache holds its rows.
 enum CacheKind { kCacheF32 = 0, kCacheBf16 = 1, kCacheQ4 = 2 };
 
@@ -38,6 +42,8 @@ struct WindowParams {
   int32_t n_sink, window;
   float scale2;                // softmax scale times log2(e)
   int64_t grid;                // workgroups
+  int32_t first, last;         // groups of KV heads' workgroups: this launch's first one, and the
+                               // call's last (a call may have more than a launch holds)
   int32_t quad;                // a workgroup takes four KV heads (one query per sequence)
   int32_t nsplit;              // parts of an item that there is room for
   int32_t plans;               // ways to cut sequences to choose from (0: none is cut)
@@ -67,7 +73,7 @@ void chunk_split(WindowParams &p, int kind, size_t scratch);
 size_t token_part_bytes(const WindowParams &p);
 size_t chunk_part_bytes(const WindowParams &p);
 hipError_t launch_token_attend(WindowParams p, int kind, bool paged, const Counting &c, hipStream_t st);
-hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st);
+hipError_t launch_chunk_attend(WindowParams p, int kind, bool paged, hipStream_t st);
 
 // Writing and reading a 4-bit cache.
 struct Q4Params {
@@ -78,6 +84,7 @@ struct Q4Params {
   const int32_t *starts;
   int64_t ncap, n_rows;
   int32_t n_pages, max_pages, batch, hkv;
+  int32_t first;               // workgroup of the call that this launch begins with
 };
 hipError_t launch_q4_append(const Q4Params &p, bool bf16, bool paged, hipStream_t st);
 hipError_t launch_q4_load(const Q4Params &p, bool bf16, bool paged, hipStream_t st);

@@ -149,13 +149,13 @@ struct ChunkRow {
 template <int ROWS, int KEYS, int UNIT, int LEAST>
 __device__ __forceinline__ bool chunk_place(const WindowParams &p, int &g, ChunkItem &it) {
   g = (int)(blockIdx.x % (uint32_t)p.hkv);
-  const int y = (int)(blockIdx.x / (uint32_t)p.hkv);
+  const int y = p.first + (int)(blockIdx.x / (uint32_t)p.hkv);
   it.s = 0;
   it.n = 1;
   // (The last row tiles first: without a window they see the most, and what ends
   // a launch should be short: 8192 tokens over themselves 575 -> 535 us, 4096
   // 169 -> 154, float32 2048 316 -> 289.)
-  if (p.plans == 0) return chunk_item<ROWS>(p, (int)(gridDim.x / (uint32_t)p.hkv) - 1 - y, it);
+  if (p.plans == 0) return chunk_item<ROWS>(p, p.last - y, it);
   auto queries = [&](int b, int &start) {
     start = (int)clamp_start(p.q_starts, b, p.n_rows);
     return max(0, (int)clamp_start(p.q_starts, b + 1, p.n_rows) - start);
@@ -732,14 +732,18 @@ size_t chunk_part_bytes(const WindowParams &p) {
   return p.plans ? (size_t)p.n_rows * p.hq * (p.nsplit * kPartStride * sizeof(float) + sizeof(int32_t)) : 0;
 }
 
-hipError_t launch_chunk_attend(const WindowParams &p, int kind, bool paged, hipStream_t st) {
+hipError_t launch_chunk_attend(WindowParams p, int kind, bool paged, hipStream_t st) {
   const bool f32 = kind == kCacheF32;
-  const int64_t grid = p.grid;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (f32 && paged) k_chunk_f32<true><<<(unsigned)grid, kBlock, 0, st>>>(p);
-  else if (f32) k_chunk_f32<false><<<(unsigned)grid, kBlock, 0, st>>>(p);
-  else if (paged) k_chunk_bf16<true><<<(unsigned)grid, kBlock, sizeof(ChunkStage), st>>>(p);
-  else k_chunk_bf16<false><<<(unsigned)grid, kBlock, sizeof(ChunkStage), st>>>(p);
+  const int64_t slots = p.grid / p.hkv, most = kMostGroups / p.hkv;
+  p.last = (int32_t)(slots - 1);
+  for (int64_t first = 0; first < slots; first += most) {
+    const unsigned n = (unsigned)(std::min(slots - first, most) * p.hkv);
+    p.first = (int32_t)first;
+    if (f32 && paged) k_chunk_f32<true><<<n, kBlock, 0, st>>>(p);
+    else if (f32) k_chunk_f32<false><<<n, kBlock, 0, st>>>(p);
+    else if (paged) k_chunk_bf16<true><<<n, kBlock, sizeof(ChunkStage), st>>>(p);
+    else k_chunk_bf16<false><<<n, kBlock, sizeof(ChunkStage), st>>>(p);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.plans == 0) return e;
   const unsigned merge = (unsigned)(chunk_tiles(p, kWaves) * p.hkv);

@@ -33,9 +33,6 @@ constexpr int kStretch = kPlan * kPerThread;      // pages counted by one workgr
 constexpr int kOneLaunch = 4 * kStretch;
 constexpr int64_t kPiece = 16 * 1024;             // bytes a workgroup copies at once
 constexpr int kMany = 1 << 29;                    // more than any number of pages
-// Workgroups of one launch, at most (a launch has less than 2^32 threads): where
-// there is more to do, each of them does several.
-constexpr int64_t kMostGroups = 1 << 23;
 
 // Scratch of one call (all int32).
 struct PageWork {

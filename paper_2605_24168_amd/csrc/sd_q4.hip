@@ -8,6 +8,8 @@
 // whole runs of 1 KB and 256 bytes.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "sd_cache.hpp"
 #include "sd_internal.hpp"
 
@@ -127,17 +129,17 @@ struct Channels {
 // the longest read back from pages 252 -> 266, contiguous 273 -> 259).
 constexpr uint32_t kXcdRuns = 16;
 template <int U>
-__device__ __forceinline__ int first_row() {
+__device__ __forceinline__ int first_row(const Q4Params &p) {
   constexpr uint32_t n = 8 * kXcdRuns;
   uint32_t i = blockIdx.x;
   if (i < gridDim.x / n * n) i = i / n * n + i % 8 * kXcdRuns + i / 8 % kXcdRuns;
-  return (int)i * U * kQ4Rows;
+  return ((int)i + p.first) * U * kQ4Rows;
 }
 
 template <int U, bool PAGED>
 __device__ __forceinline__ int64_t group_row(const Q4Params &p, const TokenRun &run, int u, int &r,
                                              TokenPlace &tp) {
-  r = first_row<U>() + u * kQ4Rows + (int)(threadIdx.x >> 4);
+  r = first_row<U>(p) + u * kQ4Rows + (int)(threadIdx.x >> 4);
   if (r >= (int)(p.n_rows * p.hkv)) {
     r = -1;
     return -1;
@@ -154,11 +156,11 @@ __global__ __launch_bounds__(kBlock) void k_q4_append(Q4Params p) {
   Channels<BF16> x[kAppendRows][2];
 #pragma unroll
   for (int u = 0; u < kAppendRows; ++u) {
-    const int r = first_row<kAppendRows>() + u * kQ4Rows + (int)(threadIdx.x >> 4);
+    const int r = first_row<kAppendRows>(p) + u * kQ4Rows + (int)(threadIdx.x >> 4);
     x[u][0].load(p.xk, min(r, rows - 1), c);
     x[u][1].load(p.xv, min(r, rows - 1), c);
   }
-  const TokenRun run = token_run(p, (int)((uint32_t)first_row<kAppendRows>() / (uint32_t)p.hkv));
+  const TokenRun run = token_run(p, (int)((uint32_t)first_row<kAppendRows>(p) / (uint32_t)p.hkv));
 #pragma unroll
   for (int u = 0; u < kAppendRows; ++u) {
     int r;
@@ -184,7 +186,7 @@ __global__ __launch_bounds__(kBlock) void k_q4_append(Q4Params p) {
 template <bool BF16, bool PAGED>
 __global__ __launch_bounds__(kBlock) void k_q4_load(Q4Params p) {
   const int c = threadIdx.x & 15;
-  const TokenRun run = token_run(p, (int)((uint32_t)first_row<kLoadRows>() / (uint32_t)p.hkv));
+  const TokenRun run = token_run(p, (int)((uint32_t)first_row<kLoadRows>(p) / (uint32_t)p.hkv));
   int r[kLoadRows];
   uint32_t codes[kLoadRows][2], scale[kLoadRows][2];
 #pragma unroll
@@ -227,22 +229,23 @@ __global__ __launch_bounds__(kBlock) void k_q4_load(Q4Params p) {
 }
 
 template <bool APPEND>
-static hipError_t launch_q4(const Q4Params &p, bool bf16, bool paged, hipStream_t st) {
+static hipError_t launch_q4(Q4Params p, bool bf16, bool paged, hipStream_t st) {
   const int64_t per = kQ4Rows * (APPEND ? kAppendRows : kLoadRows);
   const int64_t grid = (p.n_rows * p.hkv + per - 1) / per;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (grid == 0) return hipSuccess;
-  const unsigned n = (unsigned)grid;
-  if (APPEND) {
-    if (bf16 && paged) k_q4_append<true, true><<<n, kBlock, 0, st>>>(p);
-    else if (bf16) k_q4_append<true, false><<<n, kBlock, 0, st>>>(p);
-    else if (paged) k_q4_append<false, true><<<n, kBlock, 0, st>>>(p);
-    else k_q4_append<false, false><<<n, kBlock, 0, st>>>(p);
-  } else {
-    if (bf16 && paged) k_q4_load<true, true><<<n, kBlock, 0, st>>>(p);
-    else if (bf16) k_q4_load<true, false><<<n, kBlock, 0, st>>>(p);
-    else if (paged) k_q4_load<false, true><<<n, kBlock, 0, st>>>(p);
-    else k_q4_load<false, false><<<n, kBlock, 0, st>>>(p);
+  for (int64_t first = 0; first < grid; first += kMostGroups) {
+    const unsigned n = (unsigned)std::min(grid - first, kMostGroups);
+    p.first = (int32_t)first;
+    if (APPEND) {
+      if (bf16 && paged) k_q4_append<true, true><<<n, kBlock, 0, st>>>(p);
+      else if (bf16) k_q4_append<true, false><<<n, kBlock, 0, st>>>(p);
+      else if (paged) k_q4_append<false, true><<<n, kBlock, 0, st>>>(p);
+      else k_q4_append<false, false><<<n, kBlock, 0, st>>>(p);
+    } else {
+      if (bf16 && paged) k_q4_load<true, true><<<n, kBlock, 0, st>>>(p);
+      else if (bf16) k_q4_load<true, false><<<n, kBlock, 0, st>>>(p);
+      else if (paged) k_q4_load<false, true><<<n, kBlock, 0, st>>>(p);
+      else k_q4_load<false, false><<<n, kBlock, 0, st>>>(p);
+    }
   }
   return hipGetLastError();
 }

@@ -345,7 +345,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   // instead of 219, and 3 of 64K, whose 264 parts were eight too many for one
   // round, 186 instead of 136.)
   constexpr int kStep = 2 * NS;   // tiles that the waves of a head take at once
-  const int y = (int)(blockIdx.x / groups);
+  const int y = p.first + (int)(blockIdx.x / groups);
   Part part{y, 0, 0, 1, y, INT32_MAX / kStep};
   if (p.plans > 0) {
     auto steps = [&](int i, int &items) {
@@ -617,12 +617,16 @@ size_t token_part_bytes(const WindowParams &p) {
   return (size_t)p.grid * p.G * (p.quad ? 4 : 1) * kPartStride * sizeof(float);
 }
 
+// (More sequences than a launch holds are not cut: p.first is the launch's first one.)
 template <int KIND, bool PAGED, int HEADS, bool TWICE = false>
-static hipError_t launch_token(const WindowParams &p, hipStream_t st) {
+static hipError_t launch_token(WindowParams p, hipStream_t st) {
   constexpr int NW = token_waves(KIND);
-  if (p.grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  k_token_attend<KIND, PAGED, NW, HEADS, TWICE>
-      <<<(unsigned)p.grid, 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
+  const int64_t groups = p.hkv / HEADS, slots = p.grid / groups, most = kMostGroups / groups;
+  for (int64_t first = 0; first < slots; first += most) {
+    p.first = (int32_t)first;
+    k_token_attend<KIND, PAGED, NW, HEADS, TWICE>
+        <<<(unsigned)(std::min(slots - first, most) * groups), 64 * NW, token_lds_bytes(p.G, NW), st>>>(p);
+  }
   return hipGetLastError();
 }
 

@@ -64,3 +64,54 @@ def test_a_fork_of_many_rows_with_large_pages(sd, keep):
     assert np.array_equal(a.refs.cpu().numpy(), m.refs)
     assert np.array_equal(a.block_table.cpu().numpy(), m.table)
     assert np.array_equal(pool.cpu().numpy(), m.pools[0])
+
+
+def one_position(B, heads):
+    """Keys, values and queries of B sequences of one position."""
+    k, v = torch.randn((2, B, heads, 1, 128), dtype=torch.bfloat16, device="cuda")
+    return k, v, torch.randn((B, heads, 128), dtype=torch.bfloat16, device="cuda"), i32([1] * B)
+
+
+@pytest.mark.parametrize("B,heads,packed", [(65535, 129, False), (257, 65535, True)])
+def test_window_attention_of_many_sequences_and_heads(sd, B, heads, packed):
+    # 2^23 workgroups of 512 threads, or 2^24 of 256: one position, so its value
+    k, v, q, lens = one_position(B, heads)
+    starts = torch.arange(B + 1, dtype=torch.int32, device="cuda") if packed else None
+    out = torch.zeros_like(q)
+    sd.sparse_decode_window_attention(q, sd.KVCache(k=k, v=v), lens, sd.Window(), q_starts=starts, out=out)
+    assert torch.equal(out, v[:, :, 0])
+
+
+def test_four_bit_attention_of_many_sequences_and_heads(sd):
+    B, heads = 65535, 129
+    k, v, q, lens = one_position(B, heads)
+    c = sd.Q4Cache.empty(B, heads, 1)
+    sd.sparse_decode_q4_append(k[:, :, 0].contiguous(), v[:, :, 0].contiguous(), c, lens)
+    _, want = sd.sparse_decode_q4_load(c, lens)
+    out = torch.zeros_like(q)
+    sd.sparse_decode_q4_attention(q, c, lens, out=out)
+    assert torch.equal(out, want)
+
+
+def test_many_rows_appended_and_read_back(sd):
+    # 2^28 rows read back (2^24 workgroups), most of them from before the sequence.
+    heads, T, L = 16, (1 << 24) + 77, 300
+    if torch.cuda.mem_get_info()[0] < 160e9:
+        torch.cuda.empty_cache()
+        if torch.cuda.mem_get_info()[0] < 160e9:
+            pytest.skip("128 GB of rows")
+    c = sd.Q4Cache.empty(1, heads, L)
+    lens = i32([L])
+    k, v = (torch.full((T, heads, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k[-L:].normal_()
+    v[-L:].normal_()
+    half = T // 2 + 5     # (2^27 rows: in two launches, too)
+    sd.sparse_decode_q4_append(k[-half:], v[-half:], c, lens, starts=i32([0, half]))
+    want, _ = R.q4_round(k[-L:].cpu())
+    sd.sparse_decode_q4_load(c, lens, starts=i32([0, T]), k=k, v=v)
+    assert torch.equal(k[-L:].double().cpu(), want)
+    for t in (k, v):
+        assert not any(bool(t[i:min(i + (1 << 20), T - L)].any()) for i in range(0, T - L, 1 << 20))
+    assert not bool((v[-L:] == 7).any())
+    del k, v
+    torch.cuda.empty_cache()
