@@ -421,6 +421,8 @@ typedef struct {
  * step), at least 2^-95; a channel takes the level nearest to x / 2^e,
  * halfway cases the one of even index.  A group that holds a NaN or an
  * infinity reads back as NaN.
+ * Finite magnitudes from 3.5 * 2^126 on are stored as 2^128 (their nearest
+ * level), which neither float type holds: they read back as infinities.
  *   k, v     [T, Hkv, 128], float32 or bfloat16 (both the same)
  *   seq_lens device int32 [batch]: positions in the cache after the call,
  *            the new ones among them
@@ -435,8 +437,8 @@ sd_status sparse_decode_q4_append(const sd_tensor *k, const sd_tensor *v, const 
                                   int64_t batch, void *stream);
 
 /* The reverse: the last positions of each sequence as what they stand for
- * (exact in both types).  k, v [T, Hkv, 128], written, float32 or bfloat16;
- * rows and positions as in sparse_decode_q4_append.  Rows whose position is
+ * (exact in both types, an infinity from 2^128 on).  k, v [T, Hkv, 128],
+ * written, float32 or bfloat16; rows and positions as in sparse_decode_q4_append.  Rows whose position is
  * not in the cache (or whose page is not in the pool) are zeros, rows of no
  * sequence are left as they are. */
 sd_status sparse_decode_q4_load(const sd_kv4 *K, const sd_kv4 *V, const int32_t *seq_lens,

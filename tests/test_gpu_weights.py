@@ -136,3 +136,33 @@ def test_a_mean_of_equal_values_is_that_value_for_every_query(sd, layout, L, n, 
     want = value[:, :, 0].repeat_interleave(hq // hkv, 1).cuda()
     out = sd.sparse_decode_window_attention(q, cache, lens, sd.Window(softmax_scale=LN2), q_starts=starts)
     assert torch.equal(out, torch.cat((want[:1].expand(n, -1, -1), want[1:])))
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf])
+@pytest.mark.parametrize("L", [1, 31])
+def test_an_infinite_value_is_an_infinite_mean(sd, L, bad):
+    # (a weight's second number may be nothing, which an infinity would make a NaN)
+    k, v, _ = equal_values(1, 2, L, L)
+    for at in (0, L // 2, L - 1):
+        v[:, 1, at, 7] = bad
+    lens = torch.tensor([L], dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 8, 128), dtype=torch.bfloat16, device="cuda")
+    q[..., :2] = 1
+    starts = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for packed in (None, starts):
+        out = sd.sparse_decode_window_attention(q, sd.KVCache(k=k, v=v), lens, sd.Window(softmax_scale=LN2),
+                                                q_starts=packed)
+        assert (out[:, 4:, 7] == bad).all()
+        out[:, 4:, 7] = 0
+        assert torch.isfinite(out).all()
+    for hq in (4, 32):      # up to 8 query heads for a KV head, and more
+        c = sd.Q4Cache.empty(1, 2, L)
+        c.k_scales.fill_(127)
+        c.v_scales.fill_(127)
+        c.v[0, 1, :, 3] = 0xE2 if bad < 0 else 0x62      # channel 7: +-4, channel 6: 1
+        c.v_scales[0, 1, :, 0] = 253                     # 4 * 2^126
+        q = torch.ones((1, hq, 128), dtype=torch.bfloat16, device="cuda")
+        out = sd.sparse_decode_q4_attention(q, c, lens)
+        # (31 times 2^126 is past float32 before it is divided: channel 6 is not looked at)
+        assert (out[:, hq // 2:, 7] == bad).all()
+        assert torch.isfinite(out[..., 32:]).all() and torch.isfinite(out[:, :hq // 2]).all()
