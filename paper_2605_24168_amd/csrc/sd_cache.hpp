@@ -170,8 +170,8 @@ __device__ __forceinline__ Joined join_splits(const float *pp, int64_t step, int
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float fi =
-            i0 + i < k ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (i0 + i) & 63)) : 0.f;
+        if (i0 + i >= k) break;   // (not a factor of zero: a split may hold an infinity)
+        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i0 + i));
         x = fmaf(fi, v[i].x, x);
         y = fmaf(fi, v[i].y, y);
       }

@@ -139,7 +139,7 @@ def test_a_mean_of_equal_values_is_that_value_for_every_query(sd, layout, L, n, 
 
 
 @pytest.mark.parametrize("bad", [math.inf, -math.inf])
-@pytest.mark.parametrize("L", [1, 31])
+@pytest.mark.parametrize("L", [1, 31, 700, 9000])
 def test_an_infinite_value_is_an_infinite_mean(sd, L, bad):
     # (a weight's second number may be nothing, which an infinity would make a NaN)
     k, v, _ = equal_values(1, 2, L, L)
