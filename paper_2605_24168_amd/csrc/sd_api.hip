@@ -1154,8 +1154,8 @@ struct CacheShape {
   bool paged = false;
 };
 
-// data: the rows' tensor, whose last dimension is `row`; head_dim1: KV heads
-// are dimension 1 in the paged layout too (4-bit caches).
+// t: the rows' tensor, whose last dimension is `row`; heads_first: KV heads are
+// dimension 1 in the paged layout too (4-bit caches).
 sd_status check_cache(const sd_tensor &t, int layout, int page_size, const int32_t *block_table,
                       int32_t max_pages, int64_t batch, int64_t row, bool heads_first,
                       CacheShape &c) {
@@ -1166,23 +1166,23 @@ sd_status check_cache(const sd_tensor &t, int layout, int page_size, const int32
     empty = empty || t.shape[i] == 0;
   }
   if (t.shape[3] != row) return SD_ERR_UNSUPPORTED;
+  const int64_t hkv = t.shape[layout == SD_KV_PAGED_NHD && !heads_first ? 2 : 1];
+  if (hkv <= 0 || hkv > 65535) return SD_ERR_INVALID_ARG;
+  c.hkv = (int)hkv;
   if (layout == SD_KV_BHND) {
     if (t.shape[0] != batch) return SD_ERR_INVALID_ARG;
-    c.hkv = (int)t.shape[1];
     c.ncap = t.shape[2];
   } else if (layout == SD_KV_PAGED_NHD) {
     if (page_size != sd::kTile) return SD_ERR_UNSUPPORTED;
     if (t.shape[heads_first ? 2 : 1] != page_size) return SD_ERR_INVALID_ARG;
     if (max_pages < 0 || (!block_table && max_pages > 0 && batch > 0)) return SD_ERR_INVALID_ARG;
     if (t.shape[0] > INT32_MAX) return SD_ERR_UNSUPPORTED;
-    c.hkv = (int)t.shape[heads_first ? 1 : 2];
     c.ncap = (int64_t)max_pages * page_size;
     c.pages = t.shape[0];
     c.paged = true;
   } else {
     return SD_ERR_INVALID_ARG;
   }
-  if (c.hkv <= 0 || c.hkv > 65535) return SD_ERR_INVALID_ARG;
   if (c.ncap > kMaxCapacity) return SD_ERR_UNSUPPORTED;
   if (!empty && (!t.data || !aligned16(t.data))) return SD_ERR_INVALID_ARG;
   if (c.paged && c.pages == 0) c.ncap = 0;  // no page to read: every sequence counts as empty
