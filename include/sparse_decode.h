@@ -359,7 +359,7 @@ sd_status sparse_decode_read_probe(const void *buf, size_t bytes, uint32_t *sink
 typedef struct {
   int32_t n_sink;        /* >= 0 */
   int32_t window;        /* >= 0 */
-  float softmax_scale;   /* > 0, or <= 0 for 1/sqrt(128) */
+  float softmax_scale;   /* > 0 and at most 2^127, or <= 0 for 1/sqrt(128) */
 } sd_window;
 
 /*

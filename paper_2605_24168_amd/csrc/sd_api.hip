@@ -1219,8 +1219,10 @@ sd_status check_pair4(const sd_kv4 *K, const sd_kv4 *V, int64_t batch, CacheShap
   return SD_OK;
 }
 
+constexpr double kLog2e = 1.4426950408889634;   // scores become exponents of two
+
 sd_status check_window(const sd_window *w) {
-  if (!w || w->n_sink < 0 || w->window < 0 || !std::isfinite(w->softmax_scale))
+  if (!w || w->n_sink < 0 || w->window < 0 || !std::isfinite((float)(w->softmax_scale * kLog2e)))
     return SD_ERR_INVALID_ARG;
   return SD_OK;
 }
@@ -1240,7 +1242,7 @@ sd::WindowParams window_params(const CacheShape &c, int64_t batch, int64_t rows,
   p.window = w ? w->window : INT32_MAX;
   const float scale =
       w && w->softmax_scale > 0.f ? w->softmax_scale : (float)(1.0 / std::sqrt((double)kHeadDim));
-  p.scale2 = (float)(scale * 1.4426950408889634);
+  p.scale2 = (float)(scale * kLog2e);
   return p;
 }
 

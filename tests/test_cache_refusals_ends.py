@@ -22,3 +22,13 @@ def test_heads_of_a_cache_that_pass_16_bits(heads):
         rows = tensor((9, 8, 128))
         args = [C.byref(rows), C.byref(rows), C.byref(cache), C.byref(cache), FAKE, FAKE, 2, None]
         assert sd.lib.sparse_decode_q4_append(*args) == INVALID
+
+
+def test_scales_that_are_no_float32_as_exponents_of_two():
+    # 2^127 log2(e) is one, the largest float32 times log2(e) is not: zero scores
+    # would become NaN.
+    for scale in (3.4e38, 2.4e38):
+        assert window_call(w=sd.SdWindow(0, 5, scale)) == INVALID
+        assert q4_call(w=sd.SdWindow(0, 5, scale)) == INVALID
+    nothing = tensor((0, 32, 128), data=None)
+    assert window_call(q=nothing, out=nothing, starts=FAKE, w=sd.SdWindow(0, 5, 2.0**127)) == 0
