@@ -1222,7 +1222,8 @@ sd_status check_pair4(const sd_kv4 *K, const sd_kv4 *V, int64_t batch, CacheShap
 constexpr double kLog2e = 1.4426950408889634;   // scores become exponents of two
 
 sd_status check_window(const sd_window *w) {
-  if (!w || w->n_sink < 0 || w->window < 0 || !std::isfinite((float)(w->softmax_scale * kLog2e)))
+  if (!w || w->n_sink < 0 || w->window < 0 || !std::isfinite(w->softmax_scale)) return SD_ERR_INVALID_ARG;
+  if (w->softmax_scale > 0.f && !std::isfinite((float)(w->softmax_scale * kLog2e)))
     return SD_ERR_INVALID_ARG;
   return SD_OK;
 }

@@ -31,4 +31,5 @@ def test_scales_that_are_no_float32_as_exponents_of_two():
         assert window_call(w=sd.SdWindow(0, 5, scale)) == INVALID
         assert q4_call(w=sd.SdWindow(0, 5, scale)) == INVALID
     nothing = tensor((0, 32, 128), data=None)
-    assert window_call(q=nothing, out=nothing, starts=FAKE, w=sd.SdWindow(0, 5, 2.0**127)) == 0
+    for scale in (2.0**127, -3.4e38):   # (below 0: the default)
+        assert window_call(q=nothing, out=nothing, starts=FAKE, w=sd.SdWindow(0, 5, scale)) == 0
