@@ -470,8 +470,6 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     add_values<KIND, TWICE>(acc, st.tile[0], st.tile[1], pw[0], pw[1]);
   };
 
-  // (Loads past the last step touch no memory, and being unconditional let the
-  // waits count which ones are due.)
   Step st[2];
   hold_pages(0);
   load(0, st[0]);
@@ -597,10 +595,15 @@ void window_split(WindowParams &p, int kind, bool paged, size_t scratch) {
   p.nsplit = kPlanSeqs * kUnits;   // (parts of an item: any number has room)
   p.part_cost = part_cost(kind);
   if (units < 1 || items > kSplitItems || p.batch > kPlanSeqs) return;
-  // Plans of as many rounds of workgroups as the items need, one more, and
-  // twice as many: more balance better where sequences differ (not where all are
-  // longer than their windows) and have few parts in one round, and cost more
-  // where there is little to do.
+  // Plans of as many rounds of workgroups as the items need, one more, and twice as
+  // many, which balance better where sequences differ: 24 contiguous ones of 100-32K
+  // take 401 us with the first plan alone and 341 with three, 128 on pages of 100-4K
+  // 269 and 229, 60 in 4 bits of 100-32K 237 and 212 (but 64 of 100-2K 73 and 81).
+  // The first alone where all are longer than their windows, as far as the width of
+  // the table tells (64 on pages of 200-65K with a window of 4096: 177 us with more
+  // plans, 173 without), where a sequence has four slots anyway (3 and 8 of 1-64K:
+  // 80 and 275 us either way), and where there is little to do (32 of 100-1K: 25.9
+  // and 23.9 us).
   const bool more = (int64_t)p.n_sink + p.window > p.ncap / 4;
   const int64_t row = (int64_t)(kPartStride * sizeof(float)) * p.G * heads;
   for (const int64_t k : {k0, k0 + 1, 2 * k0 + 1}) {
