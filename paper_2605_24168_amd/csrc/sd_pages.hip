@@ -107,9 +107,9 @@ template <bool LIVE>
 __device__ __forceinline__ bool count_stretch(const PagesParams &p, const PageWork &w, int *tmp) {
   __shared__ bool last;
   int total;
+  if (threadIdx.x == 0) call_counter(&stretches_done, w.call);
   block_excl_scan<kPlan>(__popc(stretch_bits<LIVE>(p, blockIdx.x)), tmp, &total);
   if (threadIdx.x == 0) {
-    call_counter(&stretches_done, w.call);
     __hip_atomic_store(&w.base[blockIdx.x], total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     last = counted_last(&stretches_done, gridDim.x);
