@@ -430,7 +430,7 @@ typedef struct {
  *            position, else sequence b's rows [starts[b], starts[b + 1]) go
  *            to its last positions.
  * Rows at positions below 0, on pages outside the pool, or of no sequence, are
- * not written.
+ * not written.  (A length past the capacity counts as the capacity.)
  */
 sd_status sparse_decode_q4_append(const sd_tensor *k, const sd_tensor *v, const sd_kv4 *K,
                                   const sd_kv4 *V, const int32_t *seq_lens, const int32_t *starts,

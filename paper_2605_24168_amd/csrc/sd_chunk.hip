@@ -195,8 +195,8 @@ __device__ __forceinline__ float *chunk_part(const WindowParams &p, const ChunkI
 // four matrix instructions is followed by the load that refills its operand,
 // values behind keys and the next tile's keys behind values, so that sixteen
 // loads are always under way and each has half a tile's time to arrive.
-// 1024 tokens of 32 heads over 4096 positions: 470 us, 128 TFLOP/s of the 153
-// that a large product reaches (loads left to the compiler, two under way: 561).
+// 1024 tokens of 32 heads over 4096 positions: 459-470 us, 128-131 TFLOP/s of the
+// 154 that a large product reaches (loads left to the compiler, two under way: 561).
 // ---------------------------------------------------------------------------
 constexpr int kF32Rows = 32;
 constexpr int kF32Keys = 32;
@@ -397,11 +397,12 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_f32(WindowParams p) {
 // bfloat16: the tiles go from memory straight into LDS, and a wave computes
 // the scores of one tile while it turns those of the tile before into weights,
 // so that the matrix unit and the vector unit have work at the same time.
-// 6618 tokens of 32 heads over windows of 4096: 459-479 us, 956-997 TFLOP/s of
-// the 1243 that a large product reaches, with the last round of workgroups a
-// quarter full (8192 tokens over windows of 16384: 1063).  The matrix unit is busy for 55% of the
-// time that a compute unit has work, vector instructions for as long, at 1.9 GHz:
-// the clock falls under both (float32 runs at 2.4).
+// 6618 tokens of 32 heads over windows of 4096: 471-514 us by card and clock,
+// 890-972 TFLOP/s of the 1430 that a large product reaches, with the last round of
+// workgroups a quarter full (8192 tokens over windows of 16384: 1083).  The matrix
+// unit is busy for 51% of the time that a compute unit has work, vector
+// instructions for as long, at 1.9 GHz: the clock falls under both (float32 runs at
+// 2.4).
 // ---------------------------------------------------------------------------
 struct ChunkStage {
   u32x4 k[2][kChunkKeys * 16];   // tiles of keys and values, by parity
@@ -555,9 +556,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_chunk_bf16(WindowParams p) {
   // The weights round to bfloat16, as the values are: half a step, 2^-8
   // relative at most, independent from position to position.  (The products of a
   // second number for what that leaves, as the decode form has it, would take the
-  // matrix unit half as long again: 497 -> 681 us for 6618 tokens of 32 heads over a
+  // matrix unit half as long again: 487 -> 681 us for 6618 tokens of 32 heads over a
   // window of 4096.)  The sum takes the rounded weights, so that what they add to is
-  // a mean of the values whatever they are off by (497 -> 504 us).
+  // a mean of the values whatever they are off by (463 -> 473 us).
   auto add = [&](const u32x4 *tile, f32x16 sc[2]) {
     typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
     const b16x2 ones = __builtin_bit_cast(b16x2, 0x3F803F80u);

@@ -5,9 +5,9 @@
 // Every cached row is used by the G query heads of its KV head only, so the
 // kernel is bound by reading keys and values once: 512 bytes per position and
 // KV head in bfloat16, 136 in 4 bits.  At 8 KV heads, 64 sequences on pages with
-// a window of 4096 take 171 us (6.3 TB/s, a plain read 7.3), 16 of 128K in 4
-// bits 343 us (6.7 TB/s), 32 with a window of 16K on pages in 4 bits 92 us (6.1);
-// one sequence with a window of 1020 takes 8.5 us on the device, which are the
+// a window of 4096 take 172 us (6.3 TB/s, a plain read 7.3), 16 of 128K in 4
+// bits 350 us (6.5 TB/s), 32 with a window of 16K on pages in 4 bits 94 us (6.0);
+// one sequence with a window of 1020 takes 9.6 us on the device, which are the
 // latencies of lengths, table, rows and the joining of four parts.
 //
 // A wave takes tiles of 16 positions, two at a time, straight from global
