@@ -1278,9 +1278,12 @@ char *static_scratch(size_t bytes, sd_status &st) {
 // The next call whose workgroups count themselves.  (Called with g_mu held.)
 sd::Counting next_count(void *stream) {
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  const bool captured =
-      hipStreamIsCapturing((hipStream_t)stream, &cs) == hipSuccess && cs != hipStreamCaptureStatusNone;
-  return sd::Counting{++g_counted, captured, (g_debug.load() & 128) != 0};
+  if (hipStreamIsCapturing((hipStream_t)stream, &cs) != hipSuccess) {
+    // (The default stream while another one captures: what is launched there is not captured.)
+    cs = hipStreamCaptureStatusNone;
+    (void)hipGetLastError();
+  }
+  return sd::Counting{++g_counted, cs != hipStreamCaptureStatusNone, (g_debug.load() & 128) != 0};
 }
 
 // Splits, scratch and launches of a call.
