@@ -35,6 +35,11 @@ struct DevState {
   int n_cu = 0;         // compute units (0: not queried yet)
   // Device addresses of this GPU's copies of `scratch` and `stats_dev`
   // (hipGetSymbolAddress, taken once with the device current).
+  // The graph that the last captured call of a kind went into, and its bank.
+  struct {
+    unsigned long long graph = 0;
+    int bank = 0;
+  } captured[2];
   bool symbols = false;
   void *scratch = nullptr;
   int32_t *stats = nullptr;
@@ -1275,15 +1280,26 @@ char *static_scratch(size_t bytes, sd_status &st) {
   return st ? nullptr : (char *)ds->scratch;
 }
 
-// The next call whose workgroups count themselves.  (Called with g_mu held.)
-sd::Counting next_count(void *stream) {
+// The next call whose workgroups count themselves, after static_scratch has found
+// the device.  (Called with g_mu held.)
+enum Counters { kTokenCounters = 0, kPageCounters = 1 };
+sd::Counting next_count(Counters kind, void *stream) {
+  const bool spoil = (g_debug.load() & 128) != 0;
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing((hipStream_t)stream, &cs) != hipSuccess) {
+  unsigned long long graph = 0;
+  if (hipStreamGetCaptureInfo((hipStream_t)stream, &cs, &graph) != hipSuccess) {
     // (The default stream while another one captures: what is launched there is not captured.)
     cs = hipStreamCaptureStatusNone;
     (void)hipGetLastError();
   }
-  return sd::Counting{++g_counted, cs != hipStreamCaptureStatusNone, (g_debug.load() & 128) != 0};
+  if (cs == hipStreamCaptureStatusNone) return sd::Counting{++g_counted, 0, false, spoil};
+  int dev = 0;
+  (void)hipGetDevice(&dev);
+  auto &last = g_dev[dev].captured[kind];
+  const bool first = last.bank == 0 || last.graph != graph;
+  last.graph = graph;
+  last.bank = first ? 1 : sd::next_bank(last.bank);
+  return sd::Counting{0, last.bank, first, spoil};
 }
 
 // Splits, scratch and launches of a call.
@@ -1299,9 +1315,9 @@ sd_status run_window(sd::WindowParams &p, int kind, bool paged, void *stream) {
     if (st) return st;
     if (packed) p.part_n = (int32_t *)(p.part + p.n_rows * p.hq * p.nsplit * sd::kPartStride);
   }
-  return hip_status(packed ? sd::launch_chunk_attend(p, kind, paged, (hipStream_t)stream)
-                           : sd::launch_token_attend(p, kind, paged, next_count(stream),
-                                                     (hipStream_t)stream));
+  if (packed) return hip_status(sd::launch_chunk_attend(p, kind, paged, (hipStream_t)stream));
+  const sd::Counting c = p.plans > 0 ? next_count(kTokenCounters, stream) : sd::Counting{};
+  return hip_status(sd::launch_token_attend(p, kind, paged, c, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -1494,7 +1510,7 @@ sd_status with_pages_work(int64_t n_pages, int64_t batch, void *stream, F f) {
   std::lock_guard<std::mutex> lk(g_mu);
   sd_status st = SD_OK;
   char *base = static_scratch(sd::pages_work_bytes(n_pages, batch), st);
-  return st ? st : hip_status(f(base, next_count(stream)));
+  return st ? st : hip_status(f(base, next_count(kPageCounters, stream)));
 }
 
 }  // namespace

@@ -45,6 +45,7 @@ struct PageWork {
   int32_t *hole;      // [pages / 2]: compact: holes; fork: [0, batch) a child's rank among those
                       // that get a page, [batch, ..) the page that it copies
   uint64_t call;      // see Counting
+  int32_t bank;
 };
 enum { kLimit = 0, kMoves = 1, kLive = 2 };
 
@@ -96,9 +97,12 @@ __device__ __forceinline__ uint32_t stretch_bits(const PagesParams &p, int s) {
 }
 
 // Workgroups of the counting launch that are done.
-static __device__ uint64_t stretches_done;
+static __device__ uint64_t stretches_done[kBanks];
 
-__global__ void k_pages_counter(uint64_t x) { stretches_done = x; }
+__device__ __forceinline__ void set_counter(int bank, uint64_t x) {
+  __hip_atomic_store(&stretches_done[bank], x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__global__ void k_pages_counter(int bank, uint64_t x) { set_counter(bank, x); }
 
 // Counts this workgroup's stretch; true for the workgroup that counts last,
 // which finds all counts in w.base.  (They are stored past the caches that
@@ -107,12 +111,16 @@ template <bool LIVE>
 __device__ __forceinline__ bool count_stretch(const PagesParams &p, const PageWork &w, int *tmp) {
   __shared__ bool last;
   int total;
-  if (threadIdx.x == 0) call_counter(&stretches_done, w.call);
+  uint64_t *const done = &stretches_done[w.bank];
+  if (threadIdx.x == 0) {
+    call_counter(done, w.call);
+    if (w.bank && blockIdx.x == 0) set_counter(next_bank(w.bank), 0);
+  }
   block_excl_scan<kPlan>(__popc(stretch_bits<LIVE>(p, blockIdx.x)), tmp, &total);
   if (threadIdx.x == 0) {
     __hip_atomic_store(&w.base[blockIdx.x], total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    last = counted_last(&stretches_done, gridDim.x);
+    last = counted_last(done, gridDim.x);
   }
   __syncthreads();
   return last;
@@ -533,8 +541,11 @@ __global__ __launch_bounds__(kBlock) void k_compact_move(PagesParams p, PageWork
 // ---------------------------------------------------------------------------
 static void start_count(PageWork &w, const Counting &c, hipStream_t st) {
   w.call = c.call;
-  if (c.spoil) k_pages_counter<<<1, 1, 0, st>>>(((c.call - 1) << kCountBits) + 1);
-  if (c.captured) k_pages_counter<<<1, 1, 0, st>>>(c.call << kCountBits);
+  w.bank = c.bank;
+  const auto set = [&](int bank, uint64_t x) { k_pages_counter<<<1, 1, 0, st>>>(bank, x); };
+  if (c.spoil && c.bank == 0) set(0, ((c.call - 1) << kCountBits) + 1);
+  if (c.spoil && c.first) set(1, 1), set(2, 1);
+  if (c.first) set(c.bank, 0);
 }
 
 // Workgroups of a counting launch (one at least: it also plans).

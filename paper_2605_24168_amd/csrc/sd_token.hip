@@ -319,11 +319,15 @@ __device__ __forceinline__ void store_out(const WindowParams &p, int64_t at, flo
 
 // Parts of a (sequence, group of KV heads) that are done.
 constexpr int kSplitItems = 4096;
-static __device__ uint64_t splits_done[kSplitItems];
+static __device__ uint64_t splits_done[kBanks][kSplitItems];
 
-__global__ __launch_bounds__(kBlock) void k_token_counters(int n, uint64_t x) {
-  for (int i = blockIdx.x * kBlock + threadIdx.x; i < n; i += gridDim.x * kBlock) splits_done[i] = x;
+// By all threads of a launch.
+__device__ __forceinline__ void set_counters(int bank, uint64_t x) {
+  const int all = (int)(gridDim.x * blockDim.x);
+  for (int i = (int)(blockIdx.x * blockDim.x + threadIdx.x); i < kSplitItems; i += all)
+    __hip_atomic_store(&splits_done[bank][i], x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+__global__ __launch_bounds__(kBlock) void k_token_counters(int bank, uint64_t x) { set_counters(bank, x); }
 
 // What a workgroup costs beside its tiles, in sixteenths of a step of its waves
 // (131 KB of rows and 4.8 us, or 35 KB and 1.3 us in 4 bits; 4 us beside it).
@@ -348,6 +352,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
   // instead of 219, and 3 of 64K, whose 264 parts were eight too many for one
   // round, 186 instead of 136.)
   constexpr int kStep = 2 * NS;   // tiles that the waves of a head take at once
+  if (p.bank) set_counters(next_bank(p.bank), 0);
   const int y = p.first + (int)(blockIdx.x / groups);
   Part part{y, 0, 0, 1, y, INT32_MAX / kStep};
   if (p.plans > 0) {
@@ -486,7 +491,7 @@ __global__ __launch_bounds__(64 * NW, KIND == kCacheF32 ? 1 : 2) void k_token_at
     compute(i + 1, st[1]);
   }
 
-  uint64_t *const done = &splits_done[part.n > 1 ? b * groups + g0 / HEADS : 0];
+  uint64_t *const done = &splits_done[p.bank][part.n > 1 ? b * groups + g0 / HEADS : 0];
   if (part.n > 1 && threadIdx.x == 0) call_counter(done, p.call);
 
   // Join the waves: per head a common maximum, scaled sums and outputs.
@@ -638,12 +643,13 @@ static hipError_t launch_token(WindowParams p, hipStream_t st) {
 
 hipError_t launch_token_attend(WindowParams p, int kind, bool paged, const Counting &c, hipStream_t st) {
   p.call = c.call;
-  const int items = p.plans > 0 ? p.batch * (p.hkv / (p.quad ? 4 : 1)) : 0;
-  for (const bool left : {true, false}) {
-    if (items == 0 || !(left ? c.spoil : c.captured)) continue;
-    k_token_counters<<<(unsigned)((items + kBlock - 1) / kBlock), kBlock, 0, st>>>(
-        items, left ? ((c.call - 1) << kCountBits) + 1 : c.call << kCountBits);
-  }
+  p.bank = c.bank;
+  const auto set = [&](int bank, uint64_t x) {
+    k_token_counters<<<kSplitItems / kBlock, kBlock, 0, st>>>(bank, x);
+  };
+  if (c.spoil && c.bank == 0) set(0, ((c.call - 1) << kCountBits) + 1);
+  if (c.spoil && c.first) set(1, 1), set(2, 1);
+  if (c.first) set(c.bank, 0);
   if (p.quad) return launch_token<kCacheBf16, true, 4>(p, st);
   switch (kind) {
     case kCacheF32: return paged ? launch_token<kCacheF32, true, 1>(p, st) : launch_token<kCacheF32, false, 1>(p, st);

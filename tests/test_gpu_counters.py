@@ -74,6 +74,40 @@ def test_attention_in_parts(sd, leftovers, lens, hq, hkv):
                 assert torch.equal(call(), want) and torch.equal(out, want)
 
 
+@pytest.mark.parametrize("first", [False, True])
+def test_many_calls_in_a_graph(sd, leftovers, first):
+    # Calls of different sizes, in parts and whole, that take their counters in turn;
+    # first: the graph begins with a call that needs none.
+    g = torch.Generator().manual_seed(3)
+    k, v = torch.randn((2, 6, 2, 7000, 128), generator=g).bfloat16().cuda()
+    q = torch.randn((6, 8, 128), generator=g).bfloat16().cuda()
+    calls = []
+    for n, L in ([(2, 30)] if first else []) + [(1, 7000), (6, 5000), (2, 20), (3, 6000), (6, 7000), (1, 900)]:
+        cache = sd.KVCache(k=k[:n], v=v[:n])
+        lens = i32([L - 7 * b for b in range(n)])
+        window = sd.Window(3, 12 if L < 100 else 2**31 - 1)
+        out = torch.zeros((n, 8, 128), dtype=torch.bfloat16, device="cuda")
+        calls.append((lambda o, n=n, c=cache, l=lens, w=window:
+                      sd.sparse_decode_window_attention(q[:n], c, l, w, out=o), out))
+    want = [f(torch.zeros_like(out)) for f, out in calls]
+    for on in (False, True):
+        leftovers(on)
+        graphs = [captured(lambda part=part: [f(out) for f, out in part])
+                  for part in (calls, calls[::-1], calls[1:2], calls)]
+        for step in range(3):
+            for graph in graphs:
+                for _, out in calls:
+                    out.zero_()
+                graph.replay()
+                leftovers(on and step != 1)
+                for i in (step, -1 - step):
+                    assert torch.equal(calls[i][0](torch.zeros_like(want[i])), want[i])
+                if graph is not graphs[2]:
+                    assert all(torch.equal(out, w) for (_, out), w in zip(calls, want))
+                else:
+                    assert torch.equal(calls[1][1], want[1])
+
+
 @pytest.mark.parametrize("rows,width,pages", [(3, 40, 100), (20, 300, 5000), (20, 900, 20000)])
 def test_page_calls(sd, leftovers, rows, width, pages):
     rng = np.random.default_rng(pages)
