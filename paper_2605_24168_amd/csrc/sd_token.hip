@@ -6,7 +6,7 @@
 // kernel is bound by reading keys and values once: 512 bytes per position and
 // KV head in bfloat16, 136 in 4 bits.  At 8 KV heads, 64 sequences on pages with
 // a window of 4096 take 172 us (6.3 TB/s, a plain read 7.3), 16 of 128K in 4
-// bits 350 us (6.5 TB/s), 32 with a window of 16K on pages in 4 bits 94 us (6.0);
+// bits 350-359 us (6.4-6.5 TB/s), 32 with a window of 16K on pages in 4 bits 94 us (6.0);
 // one sequence with a window of 1020 takes 9.6 us on the device, which are the
 // latencies of lengths, table, rows and the joining of four parts.
 //
